@@ -237,6 +237,82 @@ int fftsp_decompress_segments(const void* d_packed, size_t packed_bytes, float* 
                               const size_t* seg_offsets, int nseg, float theta, int bits,
                               void* d_workspace, size_t workspace_bytes, fftsp_stream_t stream);
 
+/* ---- around the codec in a training step of a language model: the embedding and the orthogonalised update ----
+ *
+ * The embedding's gradient is the part of the flat gradient that most of whose rows are zero; the update takes the
+ * flat gradient that a receiver leaves, matrix by matrix.  Unlike above, the arrays of this section need only their
+ * own element's alignment (tensors of a flat gradient begin anywhere); workspaces are 16-byte aligned.  Everything
+ * else is as stated at the top: device pointers, nothing allocated, nothing but launches on `stream`, same bytes for
+ * the same inputs.  Element types: */
+typedef enum { FFTSP_F32 = 0, FFTSP_BF16 = 1, FFTSP_F16 = 2 } fftsp_type;
+
+/* d_out[t][j] = scale * d_table[token t][j], j < width, rounded once to out_type; a token outside [0, rows) (padding is
+ * usually -1) gives a row of zeros.  Row v of the table begins at element v * table_stride, row t of the output at
+ * t * out_stride (strides >= width; elements between width and the stride are neither read nor written).
+ * token_bits: 32 or 64 (int32_t, int64_t).  ntokens = 0 does nothing.  rows, ntokens <= 2^30, width <= 2^20;
+ * FFTSP_EINVAL otherwise.  d_out must not overlap the table or the tokens (FFTSP_EINVAL). */
+int fftsp_embedding(const void* d_table, int table_type, size_t rows, uint32_t width, size_t table_stride,
+                    const void* d_tokens, int token_bits, size_t ntokens, float scale,
+                    void* d_out, int out_type, size_t out_stride, fftsp_stream_t stream);
+
+/* Its gradient with respect to the table, every row of it written:
+ *   d_table_grad[v][j] = d_base[v][j] + scale * (sum over the t with token t == v of d_out_grad[t][j]),
+ * d_base == NULL standing for zeros.  d_base has the type and stride of d_table_grad and is the same array (the sum is
+ * added in place, and only rows that have a token are touched) or does not overlap it.  Tokens outside [0, rows) give
+ * nothing.  Sums are binary32, in an order that depends on the tokens and sizes alone; one rounding to table_type.
+ * Limits as above, and ntokens <= 2^24 (FFTSP_EUNSUPPORTED).  The workspace holds fftsp_workspace_bytes_embedding(...) bytes (0 on invalid arguments); ntokens = 0
+ * needs none. */
+size_t fftsp_workspace_bytes_embedding(size_t rows, uint32_t width, size_t ntokens);
+int fftsp_embedding_gradient(const void* d_out_grad, int out_type, size_t out_stride, const void* d_tokens,
+                             int token_bits, size_t ntokens, float scale, const void* d_base, void* d_table_grad,
+                             int table_type, size_t rows, uint32_t width, size_t table_stride,
+                             void* d_workspace, size_t workspace_bytes, fftsp_stream_t stream);
+
+/* A matrix inside flat arrays: `rows` rows of `cols` values, the first at element `offset`, rows `stride` elements
+ * apart (stride >= cols).  gain: factor on its orthogonalised form (finite). */
+typedef struct fftsp_matrix {
+    uint64_t offset, stride;
+    uint32_t rows, cols;
+    float gain;
+    uint32_t reserved; /* 0 */
+} fftsp_matrix;
+
+/* Newton-Schulz orthogonalisation of every matrix G of the list, as the Muon optimiser takes it:
+ *   X = G / (|G|_F + eps), transposed if it has more rows than columns; then, for each (a, b, c) of `coefficients`,
+ *   X <- a X + (b A + c A A) X with A = X X^T;   out = gain * X (transposed back).
+ * coefficients: HOST array of 3 * nsteps floats, read before the call returns; NULL: five steps of
+ * (3.4445, -4.7750, 2.0315), nsteps is then ignored.  1 <= nsteps <= FFTSP_MAX_STEPS; they have to keep the singular
+ * values, which begin at up to 1, and the polynomials a + b s^2 + c s^4 below 15 (the default: 1.3 and 3.5), else the
+ * output is unspecified.  eps >= 0; a matrix of zeros gives zeros (with eps = 0, too).  |G|_F is taken in binary64;
+ * inside, numbers have 22 bits or more and sums are binary32, whatever the types of d_in and d_out are.
+ * Every matrix is at `offset` of d_in and of d_out; d_in == d_out is allowed where the types agree, other overlaps are
+ * not.  Matrices of a list must not share elements (FFTSP_EINVAL; columns of one array with one stride may alternate).
+ * `matrices` is a HOST array, read before the call returns; nmat = 0 does nothing.  min(rows, cols) <= 16384,
+ * max(rows, cols) <= 2^20 (FFTSP_EUNSUPPORTED).  Non-finite values make their own matrix's output unspecified.
+ * The workspace holds fftsp_workspace_bytes_orthogonal(matrices, nmat) bytes (0 on invalid arguments). */
+#define FFTSP_MAX_STEPS 16
+size_t fftsp_workspace_bytes_orthogonal(const fftsp_matrix* matrices, int nmat);
+int fftsp_orthogonal(const void* d_in, int in_type, void* d_out, int out_type, const fftsp_matrix* matrices, int nmat,
+                     const float* coefficients, int nsteps, float eps,
+                     void* d_workspace, size_t workspace_bytes, fftsp_stream_t stream);
+
+/* The momentum step round it (Sec. 4: momentum SGD on the received gradient), for every matrix of the list:
+ *   M' = beta M + G;  U = G + beta M' (nesterov != 0) or M';  O = the above of U (before its gain);
+ *   W' = (1 - lr * weight_decay) W - lr * gain * O, rounded once to weight_type.
+ * d_grad is of grad_type (a receiver's output: FFTSP_F32), momentum is binary32.  All arrays hold the matrices at the
+ * same offsets and strides; d_momentum_out may be d_momentum and d_weights_out may be d_weights (an update in place),
+ * other overlaps are not allowed.  Elements outside the matrices are neither read nor written. */
+typedef struct fftsp_step {
+    float lr, beta, weight_decay, eps; /* finite; beta in [0, 1], eps >= 0 */
+    int nesterov;
+    int nsteps;                /* as above */
+    const float* coefficients; /* HOST, as above */
+} fftsp_step;
+int fftsp_orthogonal_step(const void* d_grad, int grad_type, const float* d_momentum, float* d_momentum_out,
+                          const void* d_weights, void* d_weights_out, int weight_type,
+                          const fftsp_matrix* matrices, int nmat, const fftsp_step* step,
+                          void* d_workspace, size_t workspace_bytes, fftsp_stream_t stream);
+
 /* Synchronises `stream`'s device and reads the status word the last call on this workspace left
  * (FFTSP_OK or FFTSP_EFORMAT).  Returns FFTSP_EHIP if the copy fails. */
 int fftsp_device_status(const void* d_workspace, int* status_out);

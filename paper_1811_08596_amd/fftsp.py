@@ -24,6 +24,28 @@ class Quantizer(C.Structure):
 
 _qp = C.POINTER(Quantizer)
 
+
+class Matrix(C.Structure):
+    """fftsp_matrix: `rows` rows of `cols` values, the first at element `offset` of flat arrays, rows `stride` apart
+    (None: cols); gain: factor on the orthogonalised form."""
+    _fields_ = [("offset", C.c_uint64), ("stride", C.c_uint64), ("rows", C.c_uint32), ("cols", C.c_uint32),
+                ("gain", C.c_float), ("reserved", C.c_uint32)]
+
+    def __init__(self, offset: int, rows: int, cols: int, stride: Optional[int] = None, gain: float = 1.0):
+        super().__init__(offset, cols if stride is None else stride, rows, cols, gain, 0)
+
+
+_mp = C.POINTER(Matrix)
+
+
+class Step(C.Structure):
+    """fftsp_step"""
+    _fields_ = [("lr", C.c_float), ("beta", C.c_float), ("weight_decay", C.c_float), ("eps", C.c_float),
+                ("nesterov", C.c_int), ("nsteps", C.c_int), ("coefficients", C.POINTER(C.c_float))]
+
+
+_sp = C.POINTER(Step)
+
 SIGNATURES = {
     "fftsp_kept_per_chunk": (C.c_int, [C.c_uint32, C.c_float, C.POINTER(C.c_uint32)]),
     "fftsp_mantissa_bits": (C.c_int, [C.c_int]),
@@ -73,6 +95,17 @@ SIGNATURES = {
                                           C.c_void_p, C.c_size_t, C.c_void_p]),
     "fftsp_decompress_segments": (C.c_int, [C.c_void_p, C.c_size_t, C.c_void_p, _szp, C.c_int, C.c_float, C.c_int,
                                             C.c_void_p, C.c_size_t, C.c_void_p]),
+    "fftsp_embedding": (C.c_int, [C.c_void_p, C.c_int, C.c_size_t, C.c_uint32, C.c_size_t, C.c_void_p, C.c_int,
+                                  C.c_size_t, C.c_float, C.c_void_p, C.c_int, C.c_size_t, C.c_void_p]),
+    "fftsp_workspace_bytes_embedding": (C.c_size_t, [C.c_size_t, C.c_uint32, C.c_size_t]),
+    "fftsp_embedding_gradient": (C.c_int, [C.c_void_p, C.c_int, C.c_size_t, C.c_void_p, C.c_int, C.c_size_t, C.c_float,
+                                           C.c_void_p, C.c_void_p, C.c_int, C.c_size_t, C.c_uint32, C.c_size_t,
+                                           C.c_void_p, C.c_size_t, C.c_void_p]),
+    "fftsp_workspace_bytes_orthogonal": (C.c_size_t, [_mp, C.c_int]),
+    "fftsp_orthogonal": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_int, _mp, C.c_int, C.POINTER(C.c_float),
+                                   C.c_int, C.c_float, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "fftsp_orthogonal_step": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int,
+                                        _mp, C.c_int, _sp, C.c_void_p, C.c_size_t, C.c_void_p]),
     "fftsp_device_status": (C.c_int, [C.c_void_p, C.POINTER(C.c_int)]),
     "fftsp_profile_enable": (C.c_int, [C.c_int]),
     "fftsp_profile_report": (C.c_size_t, [C.c_char_p, C.c_size_t]),
@@ -319,6 +352,166 @@ def decompress_segments(packed, packed_nbytes: int, grad_out, seg_offsets, theta
     _check(load().fftsp_decompress_segments(_ptr(packed), packed_nbytes, _ptr(grad_out), arr, nseg, theta, bits,
                                             _ptr(workspace), _nbytes(workspace), _stream(stream)),
            "fftsp_decompress_segments")
+
+
+# ---- the embedding and the orthogonalised update: any element's alignment, rows with strides ----
+F32, BF16, F16 = range(3)
+
+
+def _type(t) -> int:
+    import torch
+    code = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{t.dtype}: float32, bfloat16 or float16 is wanted")
+    return code
+
+
+def _same_device(*tensors):
+    """The tensors' one GPU; calls are made with it as the current device and, by default, on its current stream."""
+    dev = tensors[0].device
+    for t in tensors:
+        if not t.is_cuda or t.device != dev:
+            raise ValueError("device entry points take CUDA tensors of one device")
+    return dev
+
+
+def _on(dev, stream) -> int:
+    import torch
+    return int((stream if stream is not None else torch.cuda.current_stream(dev)).cuda_stream)
+
+
+def _current(dev):
+    """a context in which `dev` is the current device"""
+    import contextlib
+
+    import torch
+    return contextlib.nullcontext() if torch.cuda.current_device() == dev.index else torch.cuda.device(dev)
+
+
+def _rows(t, width: int):
+    """(data pointer, rows, distance of rows) of a tensor whose last axis holds `width` consecutive values; more than two
+    axes have to be contiguous"""
+    if t.dim() != 2:
+        if t.dim() < 2 or not t.is_contiguous():
+            raise ValueError("rows are a 2-D tensor, or a contiguous one of more axes")
+        t = t.view(-1, t.shape[-1])
+    if t.shape[1] != width or (width > 1 and t.stride(1) != 1):
+        raise ValueError(f"rows of {width} consecutive values are wanted, got {tuple(t.shape)} with strides {t.stride()}")
+    stride = t.stride(0) if t.shape[0] > 1 else max(width, t.stride(0))
+    return t.data_ptr(), t.shape[0], stride
+
+
+def _tokens(t, count: int) -> int:
+    import torch
+    bits = {torch.int32: 32, torch.int64: 64}.get(t.dtype)
+    if bits is None:
+        raise TypeError(f"tokens are int32 or int64, got {t.dtype}")
+    if not t.is_contiguous() or t.numel() != count:
+        raise ValueError(f"{count} contiguous tokens are wanted, got {tuple(t.shape)}")
+    return bits
+
+
+def embedding(table, tokens, out, scale: float = 1.0, stream=None):
+    """out[t] = scale * table[tokens[t]]; a token outside the table gives a row of zeros.  table: [rows, width], out:
+    [number of tokens, width] (or the tokens' shape with an axis of `width` behind it); each float32, bfloat16 or float16."""
+    dev = _same_device(table, tokens, out)
+    tp, rows, ts = _rows(table, table.shape[-1])
+    op, count, os_ = _rows(out, table.shape[-1])
+    bits = _tokens(tokens, count)
+    with _current(dev):
+        _check(load().fftsp_embedding(tp, _type(table), rows, table.shape[-1], ts, tokens.data_ptr(), bits, count, scale,
+                                      op, _type(out), os_, _on(dev, stream)), "fftsp_embedding")
+
+
+def workspace_bytes_embedding(rows: int, width: int, ntokens: int) -> int:
+    return load().fftsp_workspace_bytes_embedding(rows, width, ntokens)
+
+
+def embedding_gradient(out_grad, tokens, table_grad, workspace, scale: float = 1.0, base=None, stream=None):
+    """table_grad[v] = base[v] + scale * (sum of out_grad[t] over the t with tokens[t] == v), every row written.
+    base: None (zeros), table_grad itself (added in place) or a tensor of its type and strides."""
+    width = table_grad.shape[-1]
+    dev = _same_device(table_grad, out_grad, tokens, workspace, *([] if base is None else [base]))
+    gp, count, gs = _rows(out_grad, width)
+    tp, rows, ts = _rows(table_grad, width)
+    bits = _tokens(tokens, count)
+    bp = None
+    if base is not None:
+        bp, brows, bs = _rows(base, width)
+        if brows != rows or bs != ts or base.dtype != table_grad.dtype:
+            raise ValueError("base has the shape, strides and type of table_grad")
+    with _current(dev):
+        _check(load().fftsp_embedding_gradient(gp, _type(out_grad), gs, tokens.data_ptr(), bits, count, scale, bp, tp,
+                                               _type(table_grad), rows, width, ts, _ptr(workspace), _nbytes(workspace),
+                                               _on(dev, stream)), "fftsp_embedding_gradient")
+
+
+class Matrices:
+    """A list of fftsp_matrix for the calls below, and the elements that a flat array needs to hold it."""
+
+    def __init__(self, matrices: Sequence[Matrix]):
+        self.count = len(matrices)
+        self.array = (Matrix * max(1, self.count))(*matrices) if self.count else None
+        self.end = max((m.offset + (m.rows - 1) * m.stride + m.cols for m in matrices), default=0)
+
+
+def matrices(listing: Sequence[Matrix]) -> Matrices:
+    return Matrices(listing)
+
+
+def _flat(t, listing: Matrices, name: str) -> int:
+    if not t.is_contiguous() or t.numel() < listing.end:
+        raise ValueError(f"{name}: a contiguous tensor of {listing.end} or more elements is wanted")
+    return t.data_ptr()
+
+
+def _coefficients(coefficients):
+    """[(a, b, c), ...] or None"""
+    if coefficients is None:
+        return None, 0
+    flat = [float(v) for abc in coefficients for v in abc]
+    if len(flat) != 3 * len(coefficients):
+        raise ValueError("coefficients are triples")
+    return (C.c_float * max(1, len(flat)))(*flat), len(coefficients)
+
+
+def workspace_bytes_orthogonal(listing: Matrices) -> int:
+    return load().fftsp_workspace_bytes_orthogonal(listing.array, listing.count)
+
+
+def orthogonal(x, out, listing: Matrices, workspace, coefficients=None, eps: float = 1e-7, stream=None):
+    """Newton-Schulz orthogonalisation of every matrix of `listing`, from the flat array x into the flat array out (which
+    may be x).  coefficients: (a, b, c) of every step; None: five steps of (3.4445, -4.7750, 2.0315)."""
+    dev = _same_device(x, out, workspace)
+    co, steps = _coefficients(coefficients)  # kept alive until the call returns
+    with _current(dev):
+        _check(load().fftsp_orthogonal(_flat(x, listing, "x"), _type(x), _flat(out, listing, "out"), _type(out),
+                                       listing.array, listing.count, co, steps, eps, _ptr(workspace), _nbytes(workspace),
+                                       _on(dev, stream)), "fftsp_orthogonal")
+
+
+def orthogonal_step(grad, momentum, weights, listing: Matrices, workspace, lr: float, beta: float = 0.95,
+                    weight_decay: float = 0.0, nesterov: bool = True, coefficients=None, eps: float = 1e-7,
+                    momentum_out=None, weights_out=None, stream=None):
+    """M <- beta M + G; W <- (1 - lr weight_decay) W - lr gain O(G + beta M) for every matrix of `listing` in the flat
+    arrays grad, momentum (float32) and weights; in place unless momentum_out, weights_out are given."""
+    import torch
+    momentum_out = momentum if momentum_out is None else momentum_out
+    weights_out = weights if weights_out is None else weights_out
+    dev = _same_device(grad, momentum, weights, workspace, momentum_out, weights_out)
+    if momentum.dtype != torch.float32 or momentum_out.dtype != torch.float32:
+        raise TypeError("momentum is float32")
+    if weights_out.dtype != weights.dtype:
+        raise TypeError("weights_out has the type of weights")
+    co, steps = _coefficients(coefficients)
+    step = Step(lr, beta, weight_decay, eps, 1 if nesterov else 0, steps, co)
+    with _current(dev):
+        _check(load().fftsp_orthogonal_step(_flat(grad, listing, "grad"), _type(grad), _flat(momentum, listing, "momentum"),
+                                            _flat(momentum_out, listing, "momentum_out"),
+                                            _flat(weights, listing, "weights"),
+                                            _flat(weights_out, listing, "weights_out"), _type(weights), listing.array,
+                                            listing.count, C.byref(step), _ptr(workspace), _nbytes(workspace),
+                                            _on(dev, stream)), "fftsp_orthogonal_step")
 
 
 def device_status(workspace) -> int:
