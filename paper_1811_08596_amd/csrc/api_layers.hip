@@ -90,6 +90,7 @@ int check_matrices(const fftsp_matrix* m, int count, uint64_t* first, uint64_t* 
     return FFTSP_OK;
 }
 
+static_assert(kMostSteps == FFTSP_MAX_STEPS, "one limit");
 const float kDefaultSteps[5][3] = {{3.4445f, -4.7750f, 2.0315f}, {3.4445f, -4.7750f, 2.0315f}, {3.4445f, -4.7750f, 2.0315f},
                                    {3.4445f, -4.7750f, 2.0315f}, {3.4445f, -4.7750f, 2.0315f}};
 
@@ -102,7 +103,7 @@ int check_steps(OrthogonalArgs* a, const float* coefficients, int nsteps, float 
     if (a->nsteps < 1 || a->nsteps > FFTSP_MAX_STEPS) return FFTSP_EINVAL;
     for (int i = 0; i < 3 * a->nsteps; ++i)
         if (!std::isfinite(a->coefficients[i])) return FFTSP_EINVAL;
-    return FFTSP_OK;
+    return step_bounds(a->coefficients, a->nsteps, &a->bounds) ? FFTSP_OK : FFTSP_EUNSUPPORTED;
 }
 
 int run_orthogonal(const OrthogonalArgs& a, const fftsp_matrix* m, int count, void* ws, size_t ws_bytes, fftsp_stream_t stream)

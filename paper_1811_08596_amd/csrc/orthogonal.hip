@@ -2,20 +2,27 @@
 //
 //   X = U / (|U|_F + eps), n x m with n <= m;   per step  A = X X^T,  P = a I + b A + c A A,  X <- P X;   out = gain X
 //
-// The products carry the time: per step n^2 m for A and n^3 for A A, whose results are symmetric, so that only the tiles on
-// and under the diagonal are computed and written twice, and 2 n^2 m for P X.  They run on binary16 matrix instructions
-// whose inputs carry a binary32 number in two planes: 2^12 v = hi + lo, each rounded to nearest (22 bits and the sign of lo;
-// v is 2^-24 v off, or 2^-37 where v is small), and x y = hi hi + hi lo + lo hi summed in binary32; the part left out is under
-// 2^-24 |x| |y|.  Three instructions at sixteen times the rate of the binary32 one.
+// The products carry the time.  All matrices of a phase of up to three steps are polynomials of the phase's first A, so
+// they commute, and the steps can be taken on n x n matrices alone: Q <- P Q, A <- P A P, and X <- Q X at the phase's end.
+// That is n^2 m for A and 2 n^2 m for Q X once a phase instead of once a step, and four symmetric n x n products (n^3
+// each: only tiles on and under the diagonal are computed, and written twice) a step instead of one.  A phase ends after
+// three steps because A has an absolute error of 2^-24 of its largest eigenvalue, which the small eigenvalues' growth by
+// a^2 a step turns into a relative one: 3.4445^4 2^-24 = 1e-5 after three steps, 1e-3 after five.
 //
-// Layout: a matrix that is an operand is kept as the instruction reads it, in fragments of 32 rows x 16 columns (of the
-// contracted index), 64 lanes x 8 values of hi and then of lo: 2 KB, so that every access from memory to a wave is 1 KB in one
-// piece and LDS is read without conflicts.  Fragments along the contracted index follow each other.  X is kept twice, by rows
-// (for X X^T) and by columns (for P X).  Rows and columns are padded with zeros to whole tiles of 128; every product of them is zero
-// again, so no kernel asks where a matrix ends, but the one that reads the input and the last one.
+// Products run on binary16 matrix instructions whose inputs carry a binary32 number in two planes: 2^e v = hi + lo, each
+// rounded to nearest (v is then 2^-24 v off, or 2^-(25 + e) where v is small), and x y = hi hi + hi lo + lo hi summed in
+// binary32; the part left out is under 2^-24 |x| |y|.  Three instructions at sixteen times the binary32 one's rate.  e is up to
+// 14 and follows from the coefficients: they bound the singular values of every matrix of the iteration.
+//
+// Layout: an operand is kept as the instruction reads it, in fragments of 32 rows x 16 columns (of the contracted index),
+// 64 lanes x 8 values of hi and then of lo: 2 KB, so that every access from memory to a wave is 1 KB in one piece, goes
+// straight into LDS and is read from there without conflicts.  Fragments along the contracted index follow each other.
+// X is kept twice, by rows (for X X^T) and by columns (for Q X).  Rows and columns are padded with zeros to whole tiles;
+// products of them are zero again, so no kernel asks where a matrix ends but those that read the input or write the output.
 #include "layers.h"
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 namespace fftsp {
@@ -25,33 +32,39 @@ typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 
-constexpr float kLift = 4096.f, kDrop = 1.f / 4096.f;   // planes hold 2^12 times the number
 constexpr uint32_t kFragBytes = 2048;                   // hi and lo of 32 x 16
-constexpr uint32_t kTileRows = 128;                     // of a product's tile, both ways
+constexpr uint32_t kLeastShare = 8;                     // steps that are worth a workgroup of their own
 
-// A matrix as the kernels see it.  Offsets of planes are bytes from the workspace's start.
+// n x n matrices of the iteration
+enum Square { kA, kP, kT, kQ0, kQ1, kSquares };
+
+// A matrix as the kernels see it.  Offsets are bytes from the workspace's start.
 struct Item {
     uint64_t at, stride;        // first element and distance of rows in the caller's arrays
-    uint64_t x, xt, y, yt, a, p;
+    uint64_t x[2], xt[2];       // X by rows and by columns, before and after a phase
+    uint64_t square, square_bytes;
     uint32_t rows, cols, n, m;  // n = min, m = max
-    uint32_t nt, mt;            // tiles of 128
-    uint32_t tall;              // rows > cols: the iteration has the transposed matrix
+    uint32_t nt, mt;            // tiles
     uint32_t parts;             // workgroups that sum its squares
     float gain;
-    uint32_t pad;
 };
-// what a workgroup of a launch does: first workgroup of every matrix, by kind of launch
-enum Kind { kNorm, kConvert, kSymmetric, kWide, kKinds };
+__device__ __forceinline__ bool tall(const Item& it) { return it.rows > it.cols; }
+
+// What the workgroups of a launch do: the first one of every matrix, by kind of launch.  Products are also counted in steps
+// of 16 along the contracted index.
+enum Kind { kNorm, kConvert, kTiles, kWide, kGramSteps, kSquareSteps, kChain, kKinds };
 constexpr int kItemsPerLaunch = 24;
 struct ItemTable {
     Item item[kItemsPerLaunch];
     uint32_t start[kItemsPerLaunch][kKinds];
-    uint32_t first, count, total;
+    uint32_t first, count, total, sum[kKinds];
 };
 
+// starts: [kKinds][matrices], and behind them every kind's sum
 __global__ void k_items(ItemTable t, Item* items, uint32_t* starts)
 {
     const uint32_t i = threadIdx.x;
+    if (i < kKinds) starts[(size_t)kKinds * t.total + i] = t.sum[i];
     if (i < t.count) {
         items[t.first + i] = t.item[i];
         for (int k = 0; k < kKinds; ++k) starts[(size_t)k * t.total + t.first + i] = t.start[i][k];
@@ -82,11 +95,44 @@ __device__ __forceinline__ float load_value(const void* p, int type, uint64_t i)
     if (type == 1) return to_float(static_cast<const Bf16*>(p)[i]);
     return to_float(static_cast<const F16*>(p)[i]);
 }
-__device__ __forceinline__ void store_value(void* p, int type, uint64_t i, float v)
+// up to four values behind each other
+template <typename T>
+__device__ __forceinline__ void load_some(const T* p, uint32_t n, float* v)
 {
-    if (type == 0) static_cast<float*>(p)[i] = v;
-    else if (type == 1) static_cast<Bf16*>(p)[i] = from_float<Bf16>(v);
-    else static_cast<F16*>(p)[i] = from_float<F16>(v);
+    if (n == 4) {
+        const Run<T, 4> r = load_run<T, 4>(p);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = to_float(r.v[e]);
+    } else {
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) v[e] = e < n ? to_float(p[e]) : 0.f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store_some(T* p, uint32_t n, const float* v)
+{
+    if (n == 4) {
+        Run<T, 4> r;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r.v[e] = from_float<T>(v[e]);
+        store_run<T, 4>(p, r);
+    } else {
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e)
+            if (e < n) p[e] = from_float<T>(v[e]);
+    }
+}
+__device__ __forceinline__ void load_values(const void* p, int type, uint64_t i, uint32_t n, float* v)
+{
+    if (type == 0) load_some(static_cast<const float*>(p) + i, n, v);
+    else if (type == 1) load_some(static_cast<const Bf16*>(p) + i, n, v);
+    else load_some(static_cast<const F16*>(p) + i, n, v);
+}
+__device__ __forceinline__ void store_values(void* p, int type, uint64_t i, uint32_t n, const float* v)
+{
+    if (type == 0) store_some(static_cast<float*>(p) + i, n, v);
+    else if (type == 1) store_some(static_cast<Bf16*>(p) + i, n, v);
+    else store_some(static_cast<F16*>(p) + i, n, v);
 }
 
 struct Common {
@@ -96,12 +142,13 @@ struct Common {
     const void* weights;
     void* out;
     int in_type, out_type, nesterov, step;
-    float beta, lr, decay, eps;
+    float beta, lr, decay, eps, lift;  // lift: X's planes hold so many times X before the first phase
     uint8_t* ws;
     const Item* items;
     const uint32_t* starts;  // [kKinds][count]
-    double* parts;           // [norm workgroups]
-    uint32_t count;
+    double* sums;            // [norm workgroups]
+    uint8_t* partial;        // tiles that several workgroups share: two to a workgroup, or to one of a pair of products
+    uint32_t count, tile;    // matrices; rows of a tile
 };
 
 // ---- momentum and |U|_F^2 ----
@@ -109,7 +156,7 @@ __global__ void __launch_bounds__(256) k_norm(Common c)
 {
     __shared__ double sums[4];
     uint32_t part;
-    const Item& it = c.items[find_item(c.starts + (size_t)kNorm * c.count, c.count, blockIdx.x, &part)];
+    const Item it = c.items[find_item(c.starts + (size_t)kNorm * c.count, c.count, blockIdx.x, &part)];
     double s = 0.0;
     // a workgroup has whole rows in turn
     for (uint32_t r = part; r < it.rows; r += it.parts) {
@@ -127,7 +174,7 @@ __global__ void __launch_bounds__(256) k_norm(Common c)
     for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
     if ((threadIdx.x & 63u) == 0) sums[threadIdx.x >> 6] = s;
     __syncthreads();
-    if (threadIdx.x == 0) c.parts[blockIdx.x] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+    if (threadIdx.x == 0) c.sums[blockIdx.x] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
 }
 
 __device__ __forceinline__ void split(float v, _Float16* hi, _Float16* lo)
@@ -143,25 +190,25 @@ __global__ void __launch_bounds__(256) k_convert(Common c)
     __shared__ double sums[4];
     uint32_t at;
     const uint32_t id = find_item(c.starts + (size_t)kConvert * c.count, c.count, blockIdx.x, &at);
-    const Item& it = c.items[id];
+    const Item it = c.items[id];
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
     double s = 0.0;
     const uint32_t first_part = c.starts[(size_t)kNorm * c.count + id];
-    for (uint32_t i = tid; i < it.parts; i += 256) s += c.parts[first_part + i];
+    for (uint32_t i = tid; i < it.parts; i += 256) s += c.sums[first_part + i];
     for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
     if (lane == 0) sums[wave] = s;
     __syncthreads();
     const double norm = sqrt((sums[0] + sums[1]) + (sums[2] + sums[3])) + (double)c.eps;
-    const double factor = norm > 0.0 ? (double)kLift / norm : 0.0;
+    const double factor = norm > 0.0 ? (double)c.lift / norm : 0.0;
     // tile (tn, tm) of the iteration's n x m matrix
-    const uint32_t across = it.mt * 2u, tn = at / across, tm = at - tn * across;
+    const uint32_t across = it.mt * c.tile / 64u, tn = at / across, tm = at - tn * across;
     for (uint32_t i = tid; i < 64 * 64; i += 256) {
         // consecutive lanes along the caller's rows
         const uint32_t slow = i >> 6, fast = i & 63u;
-        const uint32_t n = tn * 64 + (it.tall ? fast : slow), m = tm * 64 + (it.tall ? slow : fast);
+        const uint32_t n = tn * 64 + (tall(it) ? fast : slow), m = tm * 64 + (tall(it) ? slow : fast);
         float v = 0.f;
         if (n < it.n && m < it.m) {
-            const uint64_t e = it.at + (it.tall ? (uint64_t)m * it.stride + n : (uint64_t)n * it.stride + m);
+            const uint64_t e = it.at + (tall(it) ? (uint64_t)m * it.stride + n : (uint64_t)n * it.stride + m);
             v = load_value(c.in, c.in_type, e);
             if (c.step) {
                 const float mo = c.momentum_out[e];
@@ -169,7 +216,7 @@ __global__ void __launch_bounds__(256) k_convert(Common c)
             }
             v = (float)((double)v * factor);
         }
-        tile[it.tall ? fast : slow][it.tall ? slow : fast] = v;
+        tile[tall(it) ? fast : slow][tall(it) ? slow : fast] = v;
     }
     __syncthreads();
     // 2 x 4 fragments of each kind, two of each to a wave
@@ -186,183 +233,217 @@ __global__ void __launch_bounds__(256) k_convert(Common c)
             lo[j] = l;
         }
         const uint64_t row = (by_columns ? tm : tn) * 2u + rb, col = (by_columns ? tn : tm) * 4u + kb;
-        const uint64_t per_row = (by_columns ? it.nt : it.mt) * 8u;
-        uint8_t* dst = c.ws + (by_columns ? it.xt : it.x) + (row * per_row + col) * kFragBytes + lane * 16u;
+        const uint64_t per_row = (by_columns ? it.nt : it.mt) * (c.tile / 16u);
+        uint8_t* dst = c.ws + (by_columns ? it.xt[0] : it.x[0]) + (row * per_row + col) * kFragBytes + lane * 16u;
         *reinterpret_cast<half8*>(dst) = hi;
         *reinterpret_cast<half8*>(dst + 1024) = lo;
     }
 }
 
 // ---- products C = L R^T of fragments ----
-enum Product { kGram, kPoly, kApply, kLast };
+// A workgroup of WM x WN waves has a tile of 32 WM BM x 32 WN BN, a wave BM x BN blocks of 32 x 32.
+// STAGES steps of 16 along the contracted index are in LDS or on their way there.
+template <int WM_, int WN_, int BM_, int BN_, int STAGES_>
+struct Shape {
+    static constexpr int WM = WM_, WN = WN_, BM = BM_, BN = BN_, STAGES = STAGES_;
+    static constexpr int kWaves = WM * WN, kThreads = kWaves * 64;
+    static constexpr int kLeft = WM * BM, kRight = WN * BN;             // row blocks of a step
+    static constexpr int kPieces = (kLeft + kRight) * 2 / kWaves;       // KB that a wave brings a step
+    static constexpr uint32_t kTile = kLeft * 32;
+    static constexpr uint32_t kStage = (kLeft + kRight) * kFragBytes;
+    static constexpr uint32_t kTurn = 32 * 36 * 4;                      // a wave's part of LDS in the epilogue
+    static constexpr uint32_t kLds = std::max(kStage * STAGES, kTurn * kWaves);
+    static constexpr uint32_t kTileBytes = kTile * kTile * 4;
+    static_assert(kLeft == kRight && (kLeft + kRight) * 2 % kWaves == 0 && kPieces * (STAGES - 2) < 64, "");
+};
+using Small = Shape<2, 2, 2, 2, 3>;  // 128 x 128, three workgroups to a compute unit
+using Large = Shape<2, 4, 4, 2, 4>;  // 256 x 256, one
+
+template <int N>
+__device__ __forceinline__ void arrived()  // all but the wave's last N pieces; then everybody's
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+// 1 KB from src into LDS, 16 bytes a lane
+__device__ __forceinline__ void bring_piece(const uint8_t* src, uint32_t lane16, uint32_t lds)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + lane16), (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+}
+
+template <typename S>
+struct Accumulators {
+    float16v v[S::BM][S::BN];
+};
+
+// acc += sum over `steps` steps; left and right: fragments of the first row block and step, row_bytes to the next row block's
+template <typename S>
+__device__ __forceinline__ void multiply(Accumulators<S>& acc, uint8_t* lds, const uint8_t* left, const uint8_t* right, uint64_t left_row,
+                                         uint64_t right_row, uint32_t steps, uint32_t wave, uint32_t lane)
+{
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds + wave * (S::kPieces * 1024u);
+    const uint8_t* src[S::kPieces];
+#pragma unroll
+    for (int q = 0; q < S::kPieces; ++q) {
+        const uint32_t p = wave * S::kPieces + q, rb = p >> 1;
+        src[q] = (rb < S::kLeft ? left + rb * left_row : right + (rb - S::kLeft) * right_row) + (p & 1u) * 1024u;
+    }
+    auto bring = [&](uint32_t slot) {
+#pragma unroll
+        for (int q = 0; q < S::kPieces; ++q) {
+            bring_piece(src[q], lane * 16u, lds0 + slot * S::kStage + q * 1024u);
+            src[q] += kFragBytes;
+        }
+    };
+    for (uint32_t s = 0; s + 1 < S::STAGES && s < steps; ++s) bring(s);
+    const uint32_t wi = (wave % S::WM) * S::BM, wj = (wave / S::WM) * S::BN;
+    uint32_t slot = 0, next = S::STAGES - 1;
+    for (uint32_t k = 0; k < steps; ++k) {
+        // steps k + 1 .. k + STAGES - 2 may still be on their way
+        if (k + S::STAGES - 1 <= steps) arrived<(S::STAGES - 2) * S::kPieces>();
+        else arrived<0>();
+        if (k + S::STAGES - 1 < steps) bring(next);
+        const uint8_t* base = lds + slot * S::kStage + lane * 16u;
+        half8 lh[S::BM], ll[S::BM], rh[S::BN], rl[S::BN];
+#pragma unroll
+        for (int j = 0; j < S::BN; ++j) {
+            const uint8_t* p = base + (S::kLeft + wj + j) * kFragBytes;
+            rh[j] = *reinterpret_cast<const half8*>(p);
+            rl[j] = *reinterpret_cast<const half8*>(p + 1024);
+        }
+#pragma unroll
+        for (int i = 0; i < S::BM; ++i) {
+            const uint8_t* p = base + (wi + i) * kFragBytes;
+            lh[i] = *reinterpret_cast<const half8*>(p);
+            ll[i] = *reinterpret_cast<const half8*>(p + 1024);
+        }
+#pragma unroll
+        for (int i = 0; i < S::BM; ++i) {
+#pragma unroll
+            for (int j = 0; j < S::BN; ++j) acc.v[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lh[i], rl[j], acc.v[i][j], 0, 0, 0);
+#pragma unroll
+            for (int j = 0; j < S::BN; ++j) acc.v[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ll[i], rh[j], acc.v[i][j], 0, 0, 0);
+#pragma unroll
+            for (int j = 0; j < S::BN; ++j) acc.v[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lh[i], rh[j], acc.v[i][j], 0, 0, 0);
+        }
+        slot = slot + 1 == S::STAGES ? 0 : slot + 1;
+        next = next + 1 == S::STAGES ? 0 : next + 1;
+    }
+    arrived<0>();  // LDS is free again
+}
+
+enum Product { kGram, kPoly, kTimes, kApply, kLast };
+__host__ __device__ constexpr bool symmetric(int what) { return what == kGram || what == kPoly || what == kTimes; }
 
 struct ProductArgs {
     Common c;
-    float ca, cb, cc;   // the step's coefficients (kPoly)
-    int odd;            // X is in y, yt (and x, xt are written)
+    float scale[2];              // of the sums, to what the result's planes hold
+    float ca, cb;                // kPoly: and ca on the diagonal, cb times A's planes
+    int left[2], right[2], out[2];  // Square; a launch of kTimes has one or two products
+    int products;
+    int phase;                   // X is x[phase & 1]
+    uint32_t len;                // steps a workgroup has, of all matrices' tiles behind each other; 0: a tile a workgroup
+    uint32_t tiles;              // of one product
 };
 
-template <int WHAT>
-__global__ void __launch_bounds__(256) k_product(ProductArgs g)
+// lane l has column l % 32 of a block and rows 8 (e / 4) + 4 (l / 32) + e % 4
+template <typename S, int WHAT>
+__device__ __forceinline__ void finish(const ProductArgs& g, const Item& it, int product, Accumulators<S>& acc, uint8_t* lds, uint32_t ti,
+                                       uint32_t tj, uint32_t wave, uint32_t lane)
 {
-    constexpr bool SYMMETRIC = WHAT == kGram || WHAT == kPoly;
-    __shared__ __align__(16) uint8_t lds[2][2][16384];
-    uint32_t at;
     const Common& c = g.c;
-    const Item& it = c.items[find_item(c.starts + (size_t)(SYMMETRIC ? kSymmetric : kWide) * c.count, c.count, blockIdx.x, &at)];
-    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    uint32_t ti, tj;  // tiles of C's rows and columns
-    if (SYMMETRIC) {  // row ti has ti + 1 tiles
-        ti = (uint32_t)((sqrtf(8.f * (float)at + 1.f) - 1.f) * 0.5f);
-        while (ti * (ti + 1) / 2 > at) --ti;
-        while ((ti + 1) * (ti + 2) / 2 <= at) ++ti;
-        tj = at - ti * (ti + 1) / 2;
-    } else {
-        tj = at / it.nt;
-        ti = at - tj * it.nt;
-    }
-    const uint32_t contracted = WHAT == kGram ? it.m : it.n;
-    const uint32_t per_row = (WHAT == kGram ? it.mt : it.nt) * 8u;  // fragments along the contracted index
-    const uint64_t xs = g.odd ? it.y : it.x, xts = g.odd ? it.yt : it.xt;
-    const uint8_t* left = c.ws + (WHAT == kGram ? xs : WHAT == kPoly ? it.a : it.p) + (uint64_t)ti * 4u * per_row * kFragBytes + tid * 16u;
-    const uint8_t* right = c.ws + (WHAT == kGram ? xs : WHAT == kPoly ? it.a : xts) + (uint64_t)tj * 4u * per_row * kFragBytes + tid * 16u;
-    const uint32_t steps = (contracted + 31u) / 32u;
-    const uint64_t block = (uint64_t)per_row * kFragBytes;
-
-    float16v acc[2][2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-
-    uint4 sl[4], sr[4];
-    auto fetch = [&](uint32_t k) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            sl[i] = *reinterpret_cast<const uint4*>(left + i * block + (uint64_t)k * (2 * kFragBytes));
-            sr[i] = *reinterpret_cast<const uint4*>(right + i * block + (uint64_t)k * (2 * kFragBytes));
-        }
-    };
-    auto stage = [&](uint32_t b) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            *reinterpret_cast<uint4*>(&lds[b][0][i * 4096 + tid * 16]) = sl[i];
-            *reinterpret_cast<uint4*>(&lds[b][1][i * 4096 + tid * 16]) = sr[i];
-        }
-    };
-    const uint32_t wi = (wave & 1u) * 2u, wj = (wave >> 1) * 2u;  // the wave's 32-blocks
-    fetch(0);
-    stage(0);
-    __syncthreads();
-    for (uint32_t k = 0; k < steps; ++k) {
-        const uint32_t b = k & 1u;
-        if (k + 1 < steps) fetch(k + 1);
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            half8 lh[2], ll[2], rh[2], rl[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint8_t* pl = &lds[b][0][(wi + i) * 4096 + kb * kFragBytes + lane * 16];
-                const uint8_t* pr = &lds[b][1][(wj + i) * 4096 + kb * kFragBytes + lane * 16];
-                lh[i] = *reinterpret_cast<const half8*>(pl);
-                ll[i] = *reinterpret_cast<const half8*>(pl + 1024);
-                rh[i] = *reinterpret_cast<const half8*>(pr);
-                rl[i] = *reinterpret_cast<const half8*>(pr + 1024);
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lh[i], rl[j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ll[i], rh[j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lh[i], rh[j], acc[i][j], 0, 0, 0);
-                }
-        }
-        if (k + 1 < steps) stage(b ^ 1u);
-        __syncthreads();
-    }
-
-    // lane l has column l % 32 of a block and rows 8 (e / 4) + 4 (l / 32) + e % 4
+    const uint32_t wi = (wave % S::WM) * S::BM, wj = (wave / S::WM) * S::BN;
     const uint32_t col = lane & 31u, half = lane >> 5;
-    if (WHAT == kLast) {
+    uint32_t* turn = reinterpret_cast<uint32_t*>(lds + wave * S::kTurn);
+    constexpr uint32_t kBlocks = S::kTile / 32u;  // of a tile's side
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < S::BM; ++i)
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < S::BN; ++j) {
+            const uint32_t bi = ti * kBlocks + wi + i, bj = tj * kBlocks + wj + j;
+            if constexpr (WHAT == kLast) {
+                // through LDS, so that lanes go along the caller's rows
+                const bool t = tall(it);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const uint32_t n = ti * kTileRows + (wi + i) * 32 + 8 * (e / 4) + 4 * half + e % 4;
-                    const uint32_t m = tj * kTileRows + (wj + j) * 32 + col;
-                    if (n >= it.n || m >= it.m) continue;
-                    const uint64_t el = it.at + (it.tall ? (uint64_t)m * it.stride + n : (uint64_t)n * it.stride + m);
-                    float v = it.gain * (acc[i][j][e] * (kDrop * kDrop));
-                    if (c.step) v = fmaf(-c.lr, v, c.decay * load_value(c.weights, c.out_type, el));
-                    store_value(c.out, c.out_type, el, v);
+                    const uint32_t r = 8 * (e / 4) + 4 * half + e % 4;
+                    turn[t ? col * 36u + r : r * 36u + col] = __float_as_uint(it.gain * (acc.v[i][j][e] * g.scale[0]));
                 }
-        return;
-    }
-    // the other orientation goes through LDS, 32 x 32 at a time, hi and lo of a value in one word
-    uint32_t* turn = reinterpret_cast<uint32_t*>(&lds[0][0][0]) + wave * (32 * 36);
-    uint8_t* direct = c.ws + (WHAT == kGram ? it.a : WHAT == kPoly ? it.p : g.odd ? it.xt : it.yt);  // rows: C's columns
-    uint8_t* turned = c.ws + (WHAT == kGram ? it.a : WHAT == kPoly ? it.p : g.odd ? it.x : it.y);
-    const uint32_t direct_row = it.nt * 8u, turned_row = (SYMMETRIC ? it.nt : it.mt) * 8u;
+                __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+                __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t slow = q * 8u + (lane >> 3), fast = (lane & 7u) * 4u;
+                    const uint32_t row = (t ? bj : bi) * 32u + slow, first = (t ? bi : bj) * 32u + fast;
+                    float v[4];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const uint32_t bi = ti * 4u + wi + i, bj = tj * 4u + wj + j;
+                    for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(turn[slow * 36u + fast + e]);
+                    if (row < it.rows && first < it.cols) {
+                        const uint64_t el = it.at + (uint64_t)row * it.stride + first;
+                        const uint32_t there = min(4u, it.cols - first);
+                        if (c.step) {
+                            float w[4];
+                            load_values(c.weights, c.out_type, el, there, w);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                half4 hi, lo;
-                const uint64_t frag = (uint64_t)bj * direct_row + bi * 2u + q / 2;
-                const uint32_t in_frag = (col + 32u * (q & 1)) * 16u + half * 8u;
-                half4 ah, al;
-                if (WHAT == kPoly) {
-                    const uint8_t* src = c.ws + it.a + frag * kFragBytes + in_frag;
-                    ah = *reinterpret_cast<const half4*>(src);
-                    al = *reinterpret_cast<const half4*>(src + 1024);
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float v = acc[i][j][q * 4 + e] * kDrop;
-                    if (WHAT == kPoly) {
-                        v = fmaf(g.cc, v, g.cb * ((float)ah[e] + (float)al[e]));
-                        if (bi == bj && col == 8u * q + 4u * half + e) v += g.ca * kLift;
+                            for (int e = 0; e < 4; ++e) v[e] = fmaf(-c.lr, v[e], c.decay * w[e]);
+                        }
+                        store_values(c.out, c.out_type, el, there, v);
                     }
-                    _Float16 h, l;
-                    split(v, &h, &l);
-                    hi[e] = h;
-                    lo[e] = l;
-                    uint16_t hb, lb;
-                    __builtin_memcpy(&hb, &h, 2);
-                    __builtin_memcpy(&lb, &l, 2);
-                    turn[(8 * q + 4 * half + e) * 36 + col] = (uint32_t)hb | (uint32_t)lb << 16;
                 }
-                uint8_t* dst = direct + frag * kFragBytes + in_frag;
-                *reinterpret_cast<half4*>(dst) = hi;
-                *reinterpret_cast<half4*>(dst + 1024) = lo;
-            }
-            __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            if (!SYMMETRIC || ti != tj) {
+            } else {
+                const int out = g.out[product];
+                uint8_t* direct = c.ws + (symmetric(WHAT) ? it.square + out * it.square_bytes : it.xt[~g.phase & 1]);  // rows: C's columns
+                uint8_t* turned = c.ws + (symmetric(WHAT) ? it.square + out * it.square_bytes : it.x[~g.phase & 1]);
+                const uint32_t direct_row = it.nt * (S::kTile / 16u), turned_row = (symmetric(WHAT) ? it.nt : it.mt) * (S::kTile / 16u);
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
-                    uint32_t w[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) w[e] = turn[col * 36 + kb * 16 + half * 8 + e];
-                    uint4 hi, lo;
-                    uint32_t* ph = reinterpret_cast<uint32_t*>(&hi);
-                    uint32_t* pl = reinterpret_cast<uint32_t*>(&lo);
+                for (int q = 0; q < 4; ++q) {
+                    half4 hi, lo, ah, al;
+                    const uint64_t frag = (uint64_t)bj * direct_row + bi * 2u + q / 2;
+                    const uint32_t in_frag = (col + 32u * (q & 1)) * 16u + half * 8u;
+                    if constexpr (WHAT == kPoly) {
+                        const uint8_t* src = c.ws + it.square + kA * it.square_bytes + frag * kFragBytes + in_frag;
+                        ah = *reinterpret_cast<const half4*>(src);
+                        al = *reinterpret_cast<const half4*>(src + 1024);
+                    }
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        ph[e] = (w[2 * e] & 0xFFFFu) | w[2 * e + 1] << 16;
-                        pl[e] = w[2 * e] >> 16 | (w[2 * e + 1] & 0xFFFF0000u);
+                        float v = acc.v[i][j][q * 4 + e] * g.scale[product];
+                        if constexpr (WHAT == kPoly) {
+                            v = fmaf(g.cb, (float)ah[e] + (float)al[e], v);
+                            if (bi == bj && col == 8u * q + 4u * half + e) v += g.ca;
+                        }
+                        _Float16 h, l;
+                        split(v, &h, &l);
+                        hi[e] = h;
+                        lo[e] = l;
+                        uint16_t hb, lb;
+                        __builtin_memcpy(&hb, &h, 2);
+                        __builtin_memcpy(&lb, &l, 2);
+                        turn[(8 * q + 4 * half + e) * 36 + col] = (uint32_t)hb | (uint32_t)lb << 16;
                     }
-                    uint8_t* dst = turned + ((uint64_t)bi * turned_row + bj * 2u + kb) * kFragBytes + lane * 16u;
-                    *reinterpret_cast<uint4*>(dst) = hi;
-                    *reinterpret_cast<uint4*>(dst + 1024) = lo;
+                    uint8_t* dst = direct + frag * kFragBytes + in_frag;
+                    *reinterpret_cast<half4*>(dst) = hi;
+                    *reinterpret_cast<half4*>(dst + 1024) = lo;
+                }
+                __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                if (!symmetric(WHAT) || ti != tj) {  // the other orientation, hi and lo of a value in one word
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb) {
+                        uint32_t w[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) w[e] = turn[col * 36 + kb * 16 + half * 8 + e];
+                        uint4 hi, lo;
+                        uint32_t* ph = reinterpret_cast<uint32_t*>(&hi);
+                        uint32_t* pl = reinterpret_cast<uint32_t*>(&lo);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            ph[e] = (w[2 * e] & 0xFFFFu) | w[2 * e + 1] << 16;
+                            pl[e] = w[2 * e] >> 16 | (w[2 * e + 1] & 0xFFFF0000u);
+                        }
+                        uint8_t* dst = turned + ((uint64_t)bi * turned_row + bj * 2u + kb) * kFragBytes + lane * 16u;
+                        *reinterpret_cast<uint4*>(dst) = hi;
+                        *reinterpret_cast<uint4*>(dst + 1024) = lo;
+                    }
                 }
             }
             __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
@@ -370,57 +451,353 @@ __global__ void __launch_bounds__(256) k_product(ProductArgs g)
         }
 }
 
+__device__ __forceinline__ void tile_of(const Item& it, bool sym, uint32_t at, uint32_t* ti, uint32_t* tj)
+{
+    if (sym) {  // row ti has ti + 1 tiles
+        uint32_t t = (uint32_t)((sqrtf(8.f * (float)at + 1.f) - 1.f) * 0.5f);
+        while (t * (t + 1) / 2 > at) --t;
+        while ((t + 1) * (t + 2) / 2 <= at) ++t;
+        *ti = t;
+        *tj = at - t * (t + 1) / 2;
+    } else {
+        *tj = at / it.nt;
+        *ti = at - *tj * it.nt;
+    }
+}
+__device__ __forceinline__ uint32_t steps_of(const Item& it, int what) { return ((what == kGram ? it.m : it.n) + 15u) / 16u; }
+
+template <typename S, int WHAT>
+__device__ __forceinline__ void multiply_tile(const ProductArgs& g, const Item& it, int product, uint32_t ti, uint32_t tj, uint32_t first,
+                                              uint32_t steps, Accumulators<S>& acc, uint8_t* lds, uint32_t wave, uint32_t lane)
+{
+#pragma unroll
+    for (int i = 0; i < S::BM; ++i)
+#pragma unroll
+        for (int j = 0; j < S::BN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc.v[i][j][e] = 0.f;
+    const Common& c = g.c;
+    const uint64_t x = it.x[g.phase & 1], xt = it.xt[g.phase & 1];
+    const uint64_t row = (uint64_t)(WHAT == kGram ? it.mt : it.nt) * (S::kTile / 16u) * kFragBytes;  // bytes of a row block
+    const uint64_t l = WHAT == kGram ? x : it.square + g.left[product] * it.square_bytes;
+    const uint64_t r = WHAT == kGram ? x : WHAT == kApply || WHAT == kLast ? xt : it.square + g.right[product] * it.square_bytes;
+    multiply<S>(acc, lds, c.ws + l + (uint64_t)ti * (S::kTile / 32u) * row + (uint64_t)first * kFragBytes,
+                c.ws + r + (uint64_t)tj * (S::kTile / 32u) * row + (uint64_t)first * kFragBytes, row, row, steps, wave, lane);
+}
+
+template <typename S, int WHAT>
+__global__ void __launch_bounds__(S::kThreads, 2) k_product(ProductArgs g)
+{
+    extern __shared__ __align__(1024) uint8_t lds[];
+    const Common& c = g.c;
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Accumulators<S> acc;
+    uint32_t ti, tj, at;
+    const int product = symmetric(WHAT) && g.products > 1 ? (int)(blockIdx.x / (gridDim.x / 2)) : 0;
+    const uint32_t wg = product ? blockIdx.x - gridDim.x / 2 : blockIdx.x;
+    if (g.len == 0) {
+        const Item it = c.items[find_item(c.starts + (size_t)(symmetric(WHAT) ? kTiles : kWide) * c.count, c.count, wg, &at)];
+        tile_of(it, symmetric(WHAT), at, &ti, &tj);
+        multiply_tile<S, WHAT>(g, it, product, ti, tj, 0, steps_of(it, WHAT), acc, lds, wave, lane);
+        finish<S, WHAT>(g, it, product, acc, lds, ti, tj, wave, lane);
+        return;
+    }
+    if constexpr (symmetric(WHAT)) {
+        // steps [begin, end) of all tiles' behind each other
+        const uint32_t* starts = c.starts + (size_t)(WHAT == kGram ? kGramSteps : kSquareSteps) * c.count;
+        const uint32_t total = c.starts[(size_t)kKinds * c.count + (WHAT == kGram ? kGramSteps : kSquareSteps)];
+        uint32_t begin = wg * g.len;
+        const uint32_t end = min(begin + g.len, total);
+        bool head = true;
+        while (begin < end) {
+            const Item it = c.items[find_item(starts, c.count, begin, &at)];
+            const uint32_t per = steps_of(it, WHAT), tile = at / per, first = at - tile * per;
+            const uint32_t steps = min(per - first, end - begin);
+            tile_of(it, true, tile, &ti, &tj);
+            multiply_tile<S, WHAT>(g, it, product, ti, tj, first, steps, acc, lds, wave, lane);
+            if (steps == per) {
+                finish<S, WHAT>(g, it, product, acc, lds, ti, tj, wave, lane);
+                __syncthreads();
+            } else {
+                // a part of a tile: as the registers have it
+                float4* dst = reinterpret_cast<float4*>(c.partial + ((uint64_t)blockIdx.x * 2u + (head && first ? 0u : 1u)) * S::kTileBytes) +
+                              threadIdx.x;
+#pragma unroll
+                for (int i = 0; i < S::BM; ++i)
+#pragma unroll
+                    for (int j = 0; j < S::BN; ++j)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const float16v& v = acc.v[i][j];
+                            dst[((i * S::BN + j) * 4 + q) * S::kThreads] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+                        }
+            }
+            begin += steps;
+            head = false;
+        }
+    }
+}
+
+// tiles that several workgroups have parts of: their sum, in the order of the steps
+template <typename S, int WHAT>
+__global__ void __launch_bounds__(S::kThreads, 2) k_join(ProductArgs g)
+{
+    extern __shared__ __align__(1024) uint8_t lds[];
+    const Common& c = g.c;
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    uint32_t at, ti, tj;
+    const int product = blockIdx.x >= g.tiles;
+    const uint32_t tile = product ? blockIdx.x - g.tiles : blockIdx.x;
+    const uint32_t id = find_item(c.starts + (size_t)kTiles * c.count, c.count, tile, &at);
+    const Item it = c.items[id];
+    const uint32_t kind = WHAT == kGram ? kGramSteps : kSquareSteps;
+    const uint32_t total = c.starts[(size_t)kKinds * c.count + kind], wgs = (total + g.len - 1) / g.len;
+    const uint32_t per = steps_of(it, WHAT), begin = c.starts[(size_t)kind * c.count + id] + at * per, last = (begin + per - 1) / g.len;
+    const uint32_t first = begin / g.len;
+    if (first == last) return;
+    Accumulators<S> acc;
+#pragma unroll
+    for (int i = 0; i < S::BM; ++i)
+#pragma unroll
+        for (int j = 0; j < S::BN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc.v[i][j][e] = 0.f;
+    for (uint32_t w = first; w <= last; ++w) {
+        const float4* src = reinterpret_cast<const float4*>(c.partial + ((uint64_t)(product * wgs + w) * 2u + (w * g.len > begin ? 0u : 1u)) * S::kTileBytes) +
+                            threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < S::BM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::BN; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const float4 v = src[((i * S::BN + j) * 4 + q) * S::kThreads];
+                    acc.v[i][j][4 * q] += v.x;
+                    acc.v[i][j][4 * q + 1] += v.y;
+                    acc.v[i][j][4 * q + 2] += v.z;
+                    acc.v[i][j][4 * q + 3] += v.w;
+                }
+    }
+    tile_of(it, true, at, &ti, &tj);
+    finish<S, WHAT>(g, it, product, acc, lds, ti, tj, wave, lane);
+}
+
 // ---- host ----
+// workgroups that share tiles, at most: what the card holds at once
+uint32_t sharing_slots(uint32_t tile) { return tile == Large::kTile ? 256u : 512u; }
+
 struct Layout {
-    size_t items, starts, parts, planes, total;
-    uint32_t workgroups[kKinds];
+    size_t items, starts, sums, partial, total;
+    uint32_t tile, count[kKinds];
 };
 
+// the matrices' places; each(i, item, workgroups of the kinds before it)
 template <typename Each>
 Layout lay_out(const MatrixSpan* m, int count, Each&& each)
 {
     Layout l{};
-    uint64_t parts = 0;
-    for (int i = 0; i < count; ++i) parts += std::min<uint32_t>(m[i].rows, 256);  // at most
+    // tiles of 256 where they are enough to fill the card
+    uint64_t large = 0;
+    for (int i = 0; i < count; ++i) {
+        const uint64_t n = std::min(m[i].rows, m[i].cols), w = std::max(m[i].rows, m[i].cols);
+        large += (n / 256) * (w / 256);
+    }
+    l.tile = large >= 256 ? Large::kTile : Small::kTile;
+    uint64_t sums = 0;
+    for (int i = 0; i < count; ++i) sums += std::min<uint32_t>(m[i].rows, 256);  // at most
     size_t off = 0;
     l.items = off;  off = align256(off + (size_t)count * sizeof(Item));
-    l.starts = off; off = align256(off + (size_t)count * kKinds * 4);
-    l.parts = off;  off = align256(off + parts * 8);
-    l.planes = off;
+    l.starts = off; off = align256(off + ((size_t)count + 1) * kKinds * 4);
+    l.sums = off;   off = align256(off + sums * 8);
     for (int i = 0; i < count; ++i) {
         Item it{};
         it.at = m[i].offset;
         it.stride = m[i].stride;
         it.rows = m[i].rows;
         it.cols = m[i].cols;
-        it.tall = it.rows > it.cols;
         it.n = std::min(it.rows, it.cols);
         it.m = std::max(it.rows, it.cols);
-        it.nt = (it.n + kTileRows - 1) / kTileRows;
-        it.mt = (it.m + kTileRows - 1) / kTileRows;
+        it.nt = (it.n + l.tile - 1) / l.tile;
+        it.mt = (it.m + l.tile - 1) / l.tile;
         it.gain = m[i].gain;
-        const size_t tile = (size_t)kTileRows * kTileRows * 4, x = (size_t)it.nt * it.mt * tile, a = (size_t)it.nt * it.nt * tile;
-        it.x = off;  off += x;
-        it.xt = off; off += x;
-        it.y = off;  off += x;
-        it.yt = off; off += x;
-        it.a = off;  off += a;
-        it.p = off;  off += a;
+        const size_t tile = (size_t)l.tile * l.tile * 4, x = (size_t)it.nt * it.mt * tile;
+        for (int k = 0; k < 2; ++k) {
+            it.x[k] = off;  off += x;
+            it.xt[k] = off; off += x;
+        }
+        it.square = off;
+        it.square_bytes = (size_t)it.nt * it.nt * tile;
+        off += kSquares * it.square_bytes;
         const size_t values = (size_t)it.n * it.m;
         it.parts = (uint32_t)std::min<size_t>(std::min<size_t>(it.rows, 256), (values + 8191) / 8192);
-        const uint32_t wgs[kKinds] = {it.parts, it.nt * 2u * it.mt * 2u, it.nt * (it.nt + 1) / 2, it.nt * it.mt};
-        each(i, it, l.workgroups);
-        for (int k = 0; k < kKinds; ++k) l.workgroups[k] += wgs[k];
+        const uint32_t tiles = it.nt * (it.nt + 1) / 2, per = l.tile / 64;
+        const uint32_t wgs[kKinds] = {it.parts, it.nt * per * it.mt * per, tiles, it.nt * it.mt, tiles * ((it.m + 15) / 16), tiles * ((it.n + 15) / 16), 0};
+        each(i, it, l.count);
+        for (int k = 0; k < kKinds; ++k) l.count[k] += wgs[k];
     }
-    l.total = off;
+    l.partial = align256(off);
+    const uint32_t sharing = std::min(sharing_slots(l.tile), (std::max(l.count[kGramSteps], 2 * l.count[kSquareSteps]) + kLeastShare - 1) / kLeastShare);
+    l.total = l.partial + (size_t)sharing * 2 * l.tile * l.tile * 4;
     return l;
+}
+
+template <typename S, int WHAT>
+hipError_t launch_product(const char* name, const char* join, const ProductArgs& g, const Layout& places, hipStream_t s)
+{
+    static std::atomic<bool> ready[64] = {};  // by device
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    if (dev < 0 || dev >= 64) return hipErrorInvalidDevice;
+    if (!ready[dev]) {
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_product<S, WHAT>), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
+        if (e == hipSuccess && symmetric(WHAT))
+            e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_join<S, symmetric(WHAT) ? WHAT : kGram>), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
+        if (e != hipSuccess) return e;
+        ready[dev] = true;
+    }
+    ProductArgs a = g;
+    const uint32_t products = symmetric(WHAT) ? (uint32_t)g.products : 1u;
+    a.tiles = places.count[symmetric(WHAT) ? kTiles : kWide];
+    a.len = 0;
+    uint32_t wgs = a.tiles * products;
+    if constexpr (symmetric(WHAT)) {
+        const uint32_t total = places.count[WHAT == kGram ? kGramSteps : kSquareSteps];
+        const uint32_t slots = sharing_slots(S::kTile) / products;
+        if (a.tiles < slots) {
+            a.len = std::max(kLeastShare, (total + slots - 1) / slots);
+            wgs = (total + a.len - 1) / a.len * products;
+        }
+    }
+    FFTSP_LAUNCH(name, (k_product<S, WHAT>), dim3(wgs), dim3(S::kThreads), S::kLds, s, a);
+    if constexpr (symmetric(WHAT))
+        if (a.len) FFTSP_LAUNCH(join, (k_join<S, WHAT>), dim3(a.tiles * products), dim3(S::kThreads), S::kLds, s, a);
+    return hipGetLastError();
+}
+
+// How many times a matrix of singular values up to `bound` its planes hold: a power of two that leaves a factor of two
+// below binary16's largest number
+float lift_for(double bound)
+{
+    int e = 14;
+    while (e > -20 && std::ldexp(bound, e) > 32768.0) --e;
+    return (float)std::ldexp(1.0, e);
+}
+
+template <typename S>
+hipError_t launch_steps(const Common& c, const OrthogonalArgs& a, const StepBounds& b, const Layout& places, hipStream_t s)
+{
+    hipError_t e = hipSuccess;
+    int step = 0;
+    for (int phase = 0; phase < b.phases && e == hipSuccess; ++phase) {
+        const float lx = lift_for(b.x[phase]);
+        ProductArgs g{};
+        g.c = c;
+        g.products = 1;
+        g.phase = phase;
+        g.out[0] = kA;
+        float la = lift_for(b.a[step]), lq = 1.f;
+        g.scale[0] = la / (lx * lx);
+        e = launch_product<S, kGram>("orthogonal_gram", "orthogonal_gram_join", g, places, s);
+        int q = kQ0;
+        for (const int first = step; step < b.end[phase] && e == hipSuccess; ++step) {
+            const int p = step == first ? kQ0 : kP;
+            const float lp = lift_for(p == kP ? b.p[step] : std::max(b.p[step], b.q[step]));
+            g.products = 1;
+            g.ca = a.coefficients[3 * step] * lp;
+            g.cb = a.coefficients[3 * step + 1] * lp / la;
+            g.scale[0] = a.coefficients[3 * step + 2] * (lp / (la * la));
+            g.left[0] = g.right[0] = kA;
+            g.out[0] = p;
+            e = launch_product<S, kPoly>("orthogonal_poly", "orthogonal_poly_join", g, places, s);
+            if (e != hipSuccess) break;
+            const bool again = step + 1 < b.end[phase];
+            const float lt = lift_for(b.t[step]);
+            int k = 0;
+            if (again) {  // T = P A
+                g.left[k] = p;
+                g.right[k] = kA;
+                g.scale[k] = lt / (lp * la);
+                g.out[k++] = kT;
+            }
+            if (p == kP) {  // Q <- P Q
+                const float next = lift_for(b.q[step]);
+                g.left[k] = kP;
+                g.right[k] = q;
+                q = q == kQ0 ? kQ1 : kQ0;
+                g.scale[k] = next / (lp * lq);
+                lq = next;
+                g.out[k++] = q;
+            } else {
+                lq = lp;
+            }
+            g.products = k;
+            if (k) e = launch_product<S, kTimes>("orthogonal_times", "orthogonal_times_join", g, places, s);
+            if (again && e == hipSuccess) {  // A <- T P
+                const float next = lift_for(b.a[step + 1]);
+                g.products = 1;
+                g.left[0] = kT;
+                g.right[0] = p;
+                g.scale[0] = next / (lt * lp);
+                la = next;
+                g.out[0] = kA;
+                e = launch_product<S, kTimes>("orthogonal_times", "orthogonal_times_join", g, places, s);
+            }
+        }
+        if (e != hipSuccess) break;
+        g.left[0] = q;
+        if (phase + 1 < b.phases) {
+            g.scale[0] = lift_for(b.x[phase + 1]) / (lq * lx);
+            e = launch_product<S, kApply>("orthogonal_apply", "", g, places, s);
+        } else {
+            g.scale[0] = 1.f / (lq * lx);
+            e = launch_product<S, kLast>("orthogonal_last", "", g, places, s);
+        }
+    }
+    return e;
 }
 
 }  // namespace
 
+// The singular values of X, A, P, T = P A and the phase's Q, from a grid over those that X can begin with.
+bool step_bounds(const float* coefficients, int nsteps, StepBounds* b)
+{
+    constexpr int kGrid = 256;
+    double x[kGrid + 1], q[kGrid + 1];
+    for (int i = 0; i <= kGrid; ++i) x[i] = (double)i / kGrid;
+    b->phases = (nsteps + kPhaseSteps - 1) / kPhaseSteps;
+    int step = 0;
+    for (int phase = 0; phase < b->phases; ++phase) {
+        b->end[phase] = (nsteps * (phase + 1) + b->phases - 1) / b->phases;
+        b->x[phase] = 0.0;
+        for (int i = 0; i <= kGrid; ++i) {
+            q[i] = 1.0;
+            b->x[phase] = std::max(b->x[phase], std::fabs(x[i]));
+        }
+        for (; step < b->end[phase]; ++step) {
+            const double ca = coefficients[3 * step], cb = coefficients[3 * step + 1], cc = coefficients[3 * step + 2];
+            b->a[step] = b->p[step] = b->t[step] = b->q[step] = 0.0;
+            for (int i = 0; i <= kGrid; ++i) {
+                const double a = x[i] * x[i], p = ca + a * (cb + a * cc);
+                q[i] *= p;
+                x[i] *= p;
+                b->a[step] = std::max(b->a[step], a);
+                b->p[step] = std::max(b->p[step], std::fabs(p));
+                b->t[step] = std::max(b->t[step], std::fabs(a * p));
+                b->q[step] = std::max(b->q[step], std::fabs(q[i]));
+            }
+            const double most = std::max(std::max(b->a[step], b->p[step]), std::max(b->t[step], b->q[step]));
+            if (!(most <= kMostBound)) return false;
+        }
+    }
+    for (int i = 0; i <= kGrid; ++i)
+        if (!(std::fabs(x[i]) <= kMostBound)) return false;
+    return true;
+}
+
 size_t orthogonal_workspace(const MatrixSpan* m, int count)
 {
-    return lay_out(m, count, [](int, const Item&, const uint32_t*) {}).total;
+    return count ? lay_out(m, count, [](int, const Item&, const uint32_t*) {}).total : 0;
 }
 
 hipError_t launch_orthogonal(const OrthogonalArgs& a, const MatrixSpan* m, int count, uint8_t* ws, hipStream_t s)
@@ -430,6 +807,7 @@ hipError_t launch_orthogonal(const OrthogonalArgs& a, const MatrixSpan* m, int c
     uint32_t* starts = reinterpret_cast<uint32_t*>(ws + places.starts);
     ItemTable t{};
     t.total = (uint32_t)count;
+    for (int k = 0; k < kKinds; ++k) t.sum[k] = places.count[k];
     lay_out(m, count, [&](int i, const Item& it, const uint32_t* begun) {
         t.item[t.count] = it;
         for (int k = 0; k < kKinds; ++k) t.start[t.count][k] = begun[k];
@@ -456,18 +834,16 @@ hipError_t launch_orthogonal(const OrthogonalArgs& a, const MatrixSpan* m, int c
     c.ws = ws;
     c.items = items;
     c.starts = starts;
-    c.parts = reinterpret_cast<double*>(ws + places.parts);
+    c.sums = reinterpret_cast<double*>(ws + places.sums);
+    c.partial = ws + places.partial;
     c.count = (uint32_t)count;
-    FFTSP_LAUNCH("orthogonal_norm", k_norm, dim3(places.workgroups[kNorm]), dim3(256), 0, s, c);
-    FFTSP_LAUNCH("orthogonal_convert", k_convert, dim3(places.workgroups[kConvert]), dim3(256), 0, s, c);
-    for (int i = 0; i < a.nsteps; ++i) {
-        const ProductArgs g{c, a.coefficients[3 * i], a.coefficients[3 * i + 1], a.coefficients[3 * i + 2], i & 1};
-        FFTSP_LAUNCH("orthogonal_gram", k_product<kGram>, dim3(places.workgroups[kSymmetric]), dim3(256), 0, s, g);
-        FFTSP_LAUNCH("orthogonal_poly", k_product<kPoly>, dim3(places.workgroups[kSymmetric]), dim3(256), 0, s, g);
-        if (i + 1 < a.nsteps) FFTSP_LAUNCH("orthogonal_apply", k_product<kApply>, dim3(places.workgroups[kWide]), dim3(256), 0, s, g);
-        else FFTSP_LAUNCH("orthogonal_last", k_product<kLast>, dim3(places.workgroups[kWide]), dim3(256), 0, s, g);
-    }
-    return hipGetLastError();
+    c.tile = places.tile;
+    c.lift = lift_for(a.bounds.x[0]);
+    FFTSP_LAUNCH("orthogonal_norm", k_norm, dim3(places.count[kNorm]), dim3(256), 0, s, c);
+    FFTSP_LAUNCH("orthogonal_convert", k_convert, dim3(places.count[kConvert]), dim3(256), 0, s, c);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    return places.tile == Large::kTile ? launch_steps<Large>(c, a, a.bounds, places, s) : launch_steps<Small>(c, a, a.bounds, places, s);
 }
 
 }  // namespace fftsp

@@ -97,6 +97,8 @@ def test_orthogonal_refusals(lib):
                 dict(ms=matrices((0, 4, 5), (3, 3, 3))[0])):
         assert call(**bad) == EINVAL, bad
     assert call(wsb=need - 1) == EWORKSPACE
+    for steps in ([5000, 0, 0], [4, 0, 0] * 7, [20, 0, 0] * 3):                      # singular values or products past 4096
+        assert call(co=(C.c_float * len(steps))(*steps), steps=len(steps) // 3) == EUNSUPPORTED, steps
     assert call(ms=matrices((0, 20000, 20000))[0], n=1) == EUNSUPPORTED
     assert call(n=0) == OK and call(ms=None, n=0, x=None, out=None, ws=None) == OK
 
