@@ -110,7 +110,9 @@ int run_orthogonal(const OrthogonalArgs& a, const fftsp_matrix* m, int count, vo
 {
     const MatrixSpan* spans = reinterpret_cast<const MatrixSpan*>(m);
     if (!ws || !aligned16(ws)) return FFTSP_EINVAL;
-    if (ws_bytes < orthogonal_workspace(spans, count)) return FFTSP_EWORKSPACE;
+    const size_t need = orthogonal_workspace(spans, count);
+    if (need == 0) return FFTSP_EUNSUPPORTED;
+    if (ws_bytes < need) return FFTSP_EWORKSPACE;
     return launch_orthogonal(a, spans, count, static_cast<uint8_t*>(ws), reinterpret_cast<hipStream_t>(stream)) == hipSuccess ? FFTSP_OK
                                                                                                                            : FFTSP_EHIP;
 }

@@ -33,10 +33,16 @@ typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 
 constexpr uint32_t kFragBytes = 2048;                   // hi and lo of 32 x 16
-constexpr uint32_t kLeastShare = 8;                     // steps that are worth a workgroup of their own
+constexpr uint32_t kLeastSteps = 8, kMostSlices = 64;   // of a tile: steps that are worth a workgroup of their own; workgroups
+constexpr uint32_t kMostParts = 1024;                   // workgroups that sum a matrix's squares
 
 // n x n matrices of the iteration
 enum Square { kA, kP, kT, kQ0, kQ1, kSquares };
+
+// Launches of products by what they contract: X X^T, one or two products of n x n by n x n, and n x n by X.
+enum Class { kGrams, kSingles, kPairs, kWides, kClasses };
+// What the workgroups of a launch do: how many the matrices before each have, by kind of launch.
+enum Kind { kNorm, kConvert, kChain, kProducts, kKinds = kProducts + kClasses };
 
 // A matrix as the kernels see it.  Offsets are bytes from the workspace's start.
 struct Item {
@@ -44,27 +50,27 @@ struct Item {
     uint64_t x[2], xt[2];       // X by rows and by columns, before and after a phase
     uint64_t square, square_bytes;
     uint32_t rows, cols, n, m;  // n = min, m = max
-    uint32_t nt, mt;            // tiles
+    uint32_t nf, mf;            // fragments along n and along m that there is room for
     uint32_t parts;             // workgroups that sum its squares
     float gain;
+    uint32_t chain;             // 1: one workgroup does its phase, 2: X X^T, too
+    uint32_t pad;
 };
 __device__ __forceinline__ bool tall(const Item& it) { return it.rows > it.cols; }
+__device__ __forceinline__ uint64_t by_rows(const Item& it, int phase) { return phase & 1 ? it.x[1] : it.x[0]; }
+__device__ __forceinline__ uint64_t by_columns(const Item& it, int phase) { return phase & 1 ? it.xt[1] : it.xt[0]; }
 
-// What the workgroups of a launch do: the first one of every matrix, by kind of launch.  Products are also counted in steps
-// of 16 along the contracted index.
-enum Kind { kNorm, kConvert, kTiles, kWide, kGramSteps, kSquareSteps, kChain, kKinds };
 constexpr int kItemsPerLaunch = 24;
 struct ItemTable {
     Item item[kItemsPerLaunch];
     uint32_t start[kItemsPerLaunch][kKinds];
-    uint32_t first, count, total, sum[kKinds];
+    uint32_t first, count, total;
 };
 
-// starts: [kKinds][matrices], and behind them every kind's sum
+// starts: [kKinds][matrices]
 __global__ void k_items(ItemTable t, Item* items, uint32_t* starts)
 {
     const uint32_t i = threadIdx.x;
-    if (i < kKinds) starts[(size_t)kKinds * t.total + i] = t.sum[i];
     if (i < t.count) {
         items[t.first + i] = t.item[i];
         for (int k = 0; k < kKinds; ++k) starts[(size_t)k * t.total + t.first + i] = t.start[i][k];
@@ -147,8 +153,9 @@ struct Common {
     const Item* items;
     const uint32_t* starts;  // [kKinds][count]
     double* sums;            // [norm workgroups]
-    uint8_t* partial;        // tiles that several workgroups share: two to a workgroup, or to one of a pair of products
-    uint32_t count, tile;    // matrices; rows of a tile
+    uint8_t* partial;        // parts of tiles that several workgroups share, by workgroup
+    uint32_t* arrivals;      // of workgroups at such a tile, by the first one's number; zero between launches
+    uint32_t count, most;    // matrices; entries of arrivals
 };
 
 // ---- momentum and |U|_F^2 ----
@@ -157,6 +164,7 @@ __global__ void __launch_bounds__(256) k_norm(Common c)
     __shared__ double sums[4];
     uint32_t part;
     const Item it = c.items[find_item(c.starts + (size_t)kNorm * c.count, c.count, blockIdx.x, &part)];
+    for (uint32_t i = blockIdx.x * 256u + threadIdx.x; i < c.most; i += gridDim.x * 256u) c.arrivals[i] = 0;
     double s = 0.0;
     // a workgroup has whole rows in turn
     for (uint32_t r = part; r < it.rows; r += it.parts) {
@@ -201,7 +209,7 @@ __global__ void __launch_bounds__(256) k_convert(Common c)
     const double norm = sqrt((sums[0] + sums[1]) + (sums[2] + sums[3])) + (double)c.eps;
     const double factor = norm > 0.0 ? (double)c.lift / norm : 0.0;
     // tile (tn, tm) of the iteration's n x m matrix
-    const uint32_t across = it.mt * c.tile / 64u, tn = at / across, tm = at - tn * across;
+    const uint32_t across = (it.m + 63u) / 64u, tn = at / across, tm = at - tn * across;
     for (uint32_t i = tid; i < 64 * 64; i += 256) {
         // consecutive lanes along the caller's rows
         const uint32_t slow = i >> 6, fast = i & 63u;
@@ -221,20 +229,20 @@ __global__ void __launch_bounds__(256) k_convert(Common c)
     __syncthreads();
     // 2 x 4 fragments of each kind, two of each to a wave
     for (uint32_t f = wave; f < 16; f += 4) {
-        const bool by_columns = f >= 8;
+        const bool turned = f >= 8;
         const uint32_t rb = (f >> 2) & 1u, kb = f & 3u;
         half8 hi, lo;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const uint32_t r = rb * 32 + (lane & 31u), k = kb * 16 + (lane >> 5) * 8 + j;
             _Float16 h, l;
-            split(by_columns ? tile[k][r] : tile[r][k], &h, &l);
+            split(turned ? tile[k][r] : tile[r][k], &h, &l);
             hi[j] = h;
             lo[j] = l;
         }
-        const uint64_t row = (by_columns ? tm : tn) * 2u + rb, col = (by_columns ? tn : tm) * 4u + kb;
-        const uint64_t per_row = (by_columns ? it.nt : it.mt) * (c.tile / 16u);
-        uint8_t* dst = c.ws + (by_columns ? it.xt[0] : it.x[0]) + (row * per_row + col) * kFragBytes + lane * 16u;
+        const uint64_t row = (turned ? tm : tn) * 2u + rb, col = (turned ? tn : tm) * 4u + kb;
+        const uint64_t per_row = turned ? it.nf : it.mf;
+        uint8_t* dst = c.ws + (turned ? it.xt[0] : it.x[0]) + (row * per_row + col) * kFragBytes + lane * 16u;
         *reinterpret_cast<half8*>(dst) = hi;
         *reinterpret_cast<half8*>(dst + 1024) = lo;
     }
@@ -267,7 +275,7 @@ __device__ __forceinline__ void arrived()  // all but the wave's last N pieces; 
 // 1 KB from src into LDS, 16 bytes a lane
 __device__ __forceinline__ void bring_piece(const uint8_t* src, uint32_t lane16, uint32_t lds)
 {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + lane16), (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + lane16), (__attribute__((address_space(3))) void*)(uintptr_t)lds, 16, 0, 0);
 }
 
 template <typename S>
@@ -341,8 +349,8 @@ struct ProductArgs {
     int left[2], right[2], out[2];  // Square; a launch of kTimes has one or two products
     int products;
     int phase;                   // X is x[phase & 1]
-    uint32_t len;                // steps a workgroup has, of all matrices' tiles behind each other; 0: a tile a workgroup
-    uint32_t tiles;              // of one product
+    int cls;
+    uint32_t len;                // steps that a workgroup has at most
 };
 
 // lane l has column l % 32 of a block and rows 8 (e / 4) + 4 (l / 32) + e % 4
@@ -391,9 +399,9 @@ __device__ __forceinline__ void finish(const ProductArgs& g, const Item& it, int
                 }
             } else {
                 const int out = g.out[product];
-                uint8_t* direct = c.ws + (symmetric(WHAT) ? it.square + out * it.square_bytes : it.xt[~g.phase & 1]);  // rows: C's columns
-                uint8_t* turned = c.ws + (symmetric(WHAT) ? it.square + out * it.square_bytes : it.x[~g.phase & 1]);
-                const uint32_t direct_row = it.nt * (S::kTile / 16u), turned_row = (symmetric(WHAT) ? it.nt : it.mt) * (S::kTile / 16u);
+                uint8_t* direct = c.ws + (symmetric(WHAT) ? it.square + out * it.square_bytes : by_columns(it, g.phase + 1));  // rows: C's columns
+                uint8_t* turned = c.ws + (symmetric(WHAT) ? it.square + out * it.square_bytes : by_rows(it, g.phase + 1));
+                const uint32_t direct_row = it.nf, turned_row = symmetric(WHAT) ? it.nf : it.mf;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     half4 hi, lo, ah, al;
@@ -451,21 +459,9 @@ __device__ __forceinline__ void finish(const ProductArgs& g, const Item& it, int
         }
 }
 
-__device__ __forceinline__ void tile_of(const Item& it, bool sym, uint32_t at, uint32_t* ti, uint32_t* tj)
-{
-    if (sym) {  // row ti has ti + 1 tiles
-        uint32_t t = (uint32_t)((sqrtf(8.f * (float)at + 1.f) - 1.f) * 0.5f);
-        while (t * (t + 1) / 2 > at) --t;
-        while ((t + 1) * (t + 2) / 2 <= at) ++t;
-        *ti = t;
-        *tj = at - t * (t + 1) / 2;
-    } else {
-        *tj = at / it.nt;
-        *ti = at - *tj * it.nt;
-    }
-}
 __device__ __forceinline__ uint32_t steps_of(const Item& it, int what) { return ((what == kGram ? it.m : it.n) + 15u) / 16u; }
 
+// acc = the steps first .. first + steps - 1 of a tile
 template <typename S, int WHAT>
 __device__ __forceinline__ void multiply_tile(const ProductArgs& g, const Item& it, int product, uint32_t ti, uint32_t tj, uint32_t first,
                                               uint32_t steps, Accumulators<S>& acc, uint8_t* lds, uint32_t wave, uint32_t lane)
@@ -477,137 +473,409 @@ __device__ __forceinline__ void multiply_tile(const ProductArgs& g, const Item& 
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc.v[i][j][e] = 0.f;
     const Common& c = g.c;
-    const uint64_t x = it.x[g.phase & 1], xt = it.xt[g.phase & 1];
-    const uint64_t row = (uint64_t)(WHAT == kGram ? it.mt : it.nt) * (S::kTile / 16u) * kFragBytes;  // bytes of a row block
+    const uint64_t x = by_rows(it, g.phase), xt = by_columns(it, g.phase);
+    const uint64_t row = (uint64_t)(WHAT == kGram ? it.mf : it.nf) * kFragBytes;  // bytes of a row block
     const uint64_t l = WHAT == kGram ? x : it.square + g.left[product] * it.square_bytes;
     const uint64_t r = WHAT == kGram ? x : WHAT == kApply || WHAT == kLast ? xt : it.square + g.right[product] * it.square_bytes;
     multiply<S>(acc, lds, c.ws + l + (uint64_t)ti * (S::kTile / 32u) * row + (uint64_t)first * kFragBytes,
                 c.ws + r + (uint64_t)tj * (S::kTile / 32u) * row + (uint64_t)first * kFragBytes, row, row, steps, wave, lane);
 }
 
+// Memory that workgroups of one launch hand over: device-scope accesses, which pass the caches that are not shared
+__device__ __forceinline__ void put(uint64_t* p, float x, float y)
+{
+    __hip_atomic_store(p, (uint64_t)__float_as_uint(x) | (uint64_t)__float_as_uint(y) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 take(const uint64_t* p)
+{
+    const uint64_t v = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
+
+// A workgroup per tile, or per slice of a tile's steps where tiles have more than `len` of them.  Every workgroup of a sliced
+// tile writes its part and counts its arrival, and the last to arrive adds the parts in the order of the steps, whoever that
+// is.  Nobody waits.
 template <typename S, int WHAT>
 __global__ void __launch_bounds__(S::kThreads, 2) k_product(ProductArgs g)
 {
     extern __shared__ __align__(1024) uint8_t lds[];
+    __shared__ uint32_t before;
     const Common& c = g.c;
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    Accumulators<S> acc;
-    uint32_t ti, tj, at;
-    const int product = symmetric(WHAT) && g.products > 1 ? (int)(blockIdx.x / (gridDim.x / 2)) : 0;
-    const uint32_t wg = product ? blockIdx.x - gridDim.x / 2 : blockIdx.x;
-    if (g.len == 0) {
-        const Item it = c.items[find_item(c.starts + (size_t)(symmetric(WHAT) ? kTiles : kWide) * c.count, c.count, wg, &at)];
-        tile_of(it, symmetric(WHAT), at, &ti, &tj);
-        multiply_tile<S, WHAT>(g, it, product, ti, tj, 0, steps_of(it, WHAT), acc, lds, wave, lane);
-        finish<S, WHAT>(g, it, product, acc, lds, ti, tj, wave, lane);
-        return;
-    }
-    if constexpr (symmetric(WHAT)) {
-        // steps [begin, end) of all tiles' behind each other
-        const uint32_t* starts = c.starts + (size_t)(WHAT == kGram ? kGramSteps : kSquareSteps) * c.count;
-        const uint32_t total = c.starts[(size_t)kKinds * c.count + (WHAT == kGram ? kGramSteps : kSquareSteps)];
-        uint32_t begin = wg * g.len;
-        const uint32_t end = min(begin + g.len, total);
-        bool head = true;
-        while (begin < end) {
-            const Item it = c.items[find_item(starts, c.count, begin, &at)];
-            const uint32_t per = steps_of(it, WHAT), tile = at / per, first = at - tile * per;
-            const uint32_t steps = min(per - first, end - begin);
-            tile_of(it, true, tile, &ti, &tj);
-            multiply_tile<S, WHAT>(g, it, product, ti, tj, first, steps, acc, lds, wave, lane);
-            if (steps == per) {
-                finish<S, WHAT>(g, it, product, acc, lds, ti, tj, wave, lane);
-                __syncthreads();
-            } else {
-                // a part of a tile: as the registers have it
-                float4* dst = reinterpret_cast<float4*>(c.partial + ((uint64_t)blockIdx.x * 2u + (head && first ? 0u : 1u)) * S::kTileBytes) +
-                              threadIdx.x;
-#pragma unroll
-                for (int i = 0; i < S::BM; ++i)
-#pragma unroll
-                    for (int j = 0; j < S::BN; ++j)
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const float16v& v = acc.v[i][j];
-                            dst[((i * S::BN + j) * 4 + q) * S::kThreads] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
-                        }
-            }
-            begin += steps;
-            head = false;
-        }
-    }
-}
-
-// tiles that several workgroups have parts of: their sum, in the order of the steps
-template <typename S, int WHAT>
-__global__ void __launch_bounds__(S::kThreads, 2) k_join(ProductArgs g)
-{
-    extern __shared__ __align__(1024) uint8_t lds[];
-    const Common& c = g.c;
-    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // workgroups go round the eight XCDs: 32 tiles behind each other, which have operands in common, to each of them in turn
+    uint32_t wg = blockIdx.x;
+    if ((wg | 255u) < gridDim.x) wg = (wg & ~255u) + (wg & 7u) * 32u + (wg >> 3 & 31u);
     uint32_t at, ti, tj;
-    const int product = blockIdx.x >= g.tiles;
-    const uint32_t tile = product ? blockIdx.x - g.tiles : blockIdx.x;
-    const uint32_t id = find_item(c.starts + (size_t)kTiles * c.count, c.count, tile, &at);
-    const Item it = c.items[id];
-    const uint32_t kind = WHAT == kGram ? kGramSteps : kSquareSteps;
-    const uint32_t total = c.starts[(size_t)kKinds * c.count + kind], wgs = (total + g.len - 1) / g.len;
-    const uint32_t per = steps_of(it, WHAT), begin = c.starts[(size_t)kind * c.count + id] + at * per, last = (begin + per - 1) / g.len;
-    const uint32_t first = begin / g.len;
-    if (first == last) return;
+    const Item it = c.items[find_item(c.starts + (size_t)(kProducts + g.cls) * c.count, c.count, wg, &at)];
+    const uint32_t per = steps_of(it, WHAT), slices = (per + g.len - 1) / g.len;
+    const uint32_t nt = (it.n + S::kTile - 1) / S::kTile;
+    uint32_t tiles = nt * (nt + 1) / 2;
+    if (!symmetric(WHAT)) tiles = nt * ((it.m + S::kTile - 1) / S::kTile);
+    int product = 0;
+    if (WHAT == kTimes && at >= tiles * slices) {
+        product = 1;
+        at -= tiles * slices;
+    }
+    const uint32_t slice = at / tiles, tile = at - slice * tiles;  // workgroups of one slice behind each other
+    const uint32_t first = (uint32_t)((uint64_t)per * slice / slices), steps = (uint32_t)((uint64_t)per * (slice + 1) / slices) - first;
+    if (symmetric(WHAT)) {  // row ti has ti + 1 tiles
+        ti = (uint32_t)((sqrtf(8.f * (float)tile + 1.f) - 1.f) * 0.5f);
+        while (ti * (ti + 1) / 2 > tile) --ti;
+        while ((ti + 1) * (ti + 2) / 2 <= tile) ++ti;
+        tj = tile - ti * (ti + 1) / 2;
+    } else {
+        tj = tile / nt;
+        ti = tile - tj * nt;
+    }
+    ti = __builtin_amdgcn_readfirstlane(ti);
+    tj = __builtin_amdgcn_readfirstlane(tj);
     Accumulators<S> acc;
-#pragma unroll
-    for (int i = 0; i < S::BM; ++i)
-#pragma unroll
-        for (int j = 0; j < S::BN; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc.v[i][j][e] = 0.f;
-    for (uint32_t w = first; w <= last; ++w) {
-        const float4* src = reinterpret_cast<const float4*>(c.partial + ((uint64_t)(product * wgs + w) * 2u + (w * g.len > begin ? 0u : 1u)) * S::kTileBytes) +
-                            threadIdx.x;
+    multiply_tile<S, WHAT>(g, it, product, ti, tj, first, steps, acc, lds, wave, lane);
+    if (slices > 1) {
+        const uint32_t wg0 = wg - slice * tiles;
+        auto part = [&](uint32_t s) { return reinterpret_cast<uint64_t*>(c.partial + (uint64_t)(wg0 + s * tiles) * S::kTileBytes) + threadIdx.x; };
+        uint64_t* dst = part(slice);
 #pragma unroll
         for (int i = 0; i < S::BM; ++i)
 #pragma unroll
             for (int j = 0; j < S::BN; ++j)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const float4 v = src[((i * S::BN + j) * 4 + q) * S::kThreads];
-                    acc.v[i][j][4 * q] += v.x;
-                    acc.v[i][j][4 * q + 1] += v.y;
-                    acc.v[i][j][4 * q + 2] += v.z;
-                    acc.v[i][j][4 * q + 3] += v.w;
-                }
+                for (int q = 0; q < 8; ++q) put(dst + ((i * S::BN + j) * 8 + q) * S::kThreads, acc.v[i][j][2 * q], acc.v[i][j][2 * q + 1]);
+        arrived<0>();  // every wave's stores are where all can see them
+        uint32_t* count = c.arrivals + wg0;
+        if (threadIdx.x == 0) before = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+        if (__builtin_amdgcn_readfirstlane(before) + 1 < slices) return;
+        if (threadIdx.x == 0) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        for (uint32_t s = 0; s < slices; ++s) {
+            const uint64_t* src = part(s);
+#pragma unroll
+            for (int i = 0; i < S::BM; ++i) {
+                float2 v[S::BN][8];  // all on their way before the first is added
+#pragma unroll
+                for (int j = 0; j < S::BN; ++j)
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) v[j][q] = take(src + ((i * S::BN + j) * 8 + q) * S::kThreads);
+#pragma unroll
+                for (int j = 0; j < S::BN; ++j)
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        acc.v[i][j][2 * q] = s ? acc.v[i][j][2 * q] + v[j][q].x : v[j][q].x;
+                        acc.v[i][j][2 * q + 1] = s ? acc.v[i][j][2 * q + 1] + v[j][q].y : v[j][q].y;
+                    }
+            }
+        }
     }
-    tile_of(it, true, at, &ti, &tj);
     finish<S, WHAT>(g, it, product, acc, lds, ti, tj, wave, lane);
 }
 
-// ---- host ----
-// workgroups that share tiles, at most: what the card holds at once
-uint32_t sharing_slots(uint32_t tile) { return tile == Large::kTile ? 256u : 512u; }
+// ---- a whole phase of a small matrix (n <= 128): one workgroup, A, P and (n <= 96) Q in LDS ----
+struct ChainStep {
+    float ca, cb, poly, t, q, a;  // as in ProductArgs, for P, P A, P Q and A's
+};
+struct ChainArgs {
+    Common c;
+    ChainStep step[kPhaseSteps];
+    int steps, phase, q;  // q: where the apply looks for Q
+    float gram;
+};
+constexpr int kChainThreads = 512, kChainWaves = 8;
+constexpr uint32_t kChainMost = 128, kChainGram = 64, kChainGramSteps = 512;  // n; n and steps of X X^T that the same workgroup does
+constexpr uint32_t kChainLds = 128 * 1024;
 
-struct Layout {
-    size_t items, starts, sums, partial, total;
-    uint32_t tile, count[kKinds];
+// fragments of a matrix: row block rb, step kb
+struct Plane {
+    uint8_t* base;
+    uint32_t per_row;
+    __device__ uint8_t* frag(uint32_t rb, uint32_t kb) const { return base + ((uint64_t)rb * per_row + kb) * kFragBytes; }
 };
 
-// the matrices' places; each(i, item, workgroups of the kinds before it)
+// blocks b = w PER + e of the nb x nb ones
+template <int PER>
+__device__ __forceinline__ void chain_product(float16v (&acc)[PER], const Plane& l, const Plane& r, uint32_t nb, uint32_t steps, uint32_t wave, uint32_t lane)
+{
+#pragma unroll
+    for (int e = 0; e < PER; ++e)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) acc[e][k] = 0.f;
+    if (wave * PER >= nb * nb) return;
+    for (uint32_t k = 0; k < steps; ++k) {
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            const uint32_t b = min(wave * PER + e, nb * nb - 1), i = b / nb, j = b - i * nb;
+            const uint8_t *pl = l.frag(i, k) + lane * 16u, *pr = r.frag(j, k) + lane * 16u;
+            const half8 lh = *reinterpret_cast<const half8*>(pl), ll = *reinterpret_cast<const half8*>(pl + 1024);
+            const half8 rh = *reinterpret_cast<const half8*>(pr), rl = *reinterpret_cast<const half8*>(pr + 1024);
+            acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lh, rl, acc[e], 0, 0, 0);
+            acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ll, rh, acc[e], 0, 0, 0);
+            acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lh, rh, acc[e], 0, 0, 0);
+        }
+    }
+}
+// four values of one column to a matrix's fragments (of its transpose, which it equals)
+__device__ __forceinline__ void chain_write(const Plane& to, uint32_t i, uint32_t j, uint32_t q, const float* v, uint32_t lane)
+{
+    half4 hi, lo;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        _Float16 h, l;
+        split(v[e], &h, &l);
+        hi[e] = h;
+        lo[e] = l;
+    }
+    uint8_t* dst = to.frag(j, i * 2u + q / 2u) + ((lane & 31u) + 32u * (q & 1u)) * 16u + (lane >> 5) * 8u;
+    *reinterpret_cast<half4*>(dst) = hi;
+    *reinterpret_cast<half4*>(dst + 1024) = lo;
+}
+template <int PER>
+__device__ __forceinline__ void chain_store(const Plane& to, const float16v (&acc)[PER], float scale, uint32_t nb, uint32_t wave, uint32_t lane)
+{
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        const uint32_t b = wave * PER + e;
+        if (b >= nb * nb) continue;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            float v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = acc[e][4 * q + k] * scale;
+            chain_write(to, b / nb, b % nb, q, v, lane);
+        }
+    }
+}
+
+template <int PER>
+__device__ __forceinline__ void chain_steps(const ChainArgs& g, const Item& it, uint8_t* lds, uint32_t nb, uint32_t wave, uint32_t lane)
+{
+    const uint32_t steps = (it.n + 15u) / 16u, bytes = nb * nb * 2u * kFragBytes;
+    const Plane a{lds, 2 * nb}, p{lds + bytes, 2 * nb}, out{g.c.ws + it.square + g.q * it.square_bytes, it.nf};
+    const Plane q = nb < 4 ? Plane{lds + 2 * bytes, 2 * nb} : out;
+    for (int s = 0; s < g.steps; ++s) {
+        const ChainStep& st = g.step[s];
+        const bool again = s + 1 < g.steps;
+        {
+            float16v acc[PER];
+            chain_product<PER>(acc, a, a, nb, steps, wave, lane);
+#pragma unroll
+            for (int e = 0; e < PER; ++e) {
+                const uint32_t b = wave * PER + e, i = b / nb, j = b % nb;
+                if (b >= nb * nb) continue;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint8_t* src = a.frag(j, i * 2u + k / 2u) + ((lane & 31u) + 32u * (k & 1u)) * 16u + (lane >> 5) * 8u;
+                    const half4 ah = *reinterpret_cast<const half4*>(src), al = *reinterpret_cast<const half4*>(src + 1024);
+                    float v[4];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        v[t] = fmaf(st.cb, (float)ah[t] + (float)al[t], acc[e][4 * k + t] * st.poly);
+                        if (i == j && (lane & 31u) == 8u * k + 4u * (lane >> 5) + t) v[t] += st.ca;
+                    }
+                    if (again || s) chain_write(p, i, j, k, v, lane);
+                    if (s == 0) chain_write(again ? q : out, i, j, k, v, lane);
+                }
+            }
+        }
+        __syncthreads();
+        float16v t[PER], w[PER];
+        if (again) chain_product<PER>(t, p, a, nb, steps, wave, lane);
+        if (s) chain_product<PER>(w, p, q, nb, steps, wave, lane);
+        __syncthreads();
+        if (again) chain_store<PER>(a, t, st.t, nb, wave, lane);  // T in A's place
+        if (s) chain_store<PER>(again ? q : out, w, st.q, nb, wave, lane);
+        __syncthreads();
+        if (again) {
+            chain_product<PER>(t, a, p, nb, steps, wave, lane);
+            __syncthreads();
+            chain_store<PER>(a, t, st.a, nb, wave, lane);
+            __syncthreads();
+        }
+    }
+}
+
+// A = X X^T of n <= 32 NB: every wave has an eighth of the steps
+template <int NB>
+__device__ __forceinline__ void chain_gram(const ChainArgs& g, const Item& it, uint8_t* lds, uint32_t wave, uint32_t lane)
+{
+    float16v acc[NB][NB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    const uint32_t steps = (it.m + 15u) / 16u;
+    const Plane x{g.c.ws + by_rows(it, g.phase), it.mf};
+    constexpr uint32_t kAhead = 4;  // steps whose fragments are on their way together
+    for (uint32_t k = wave; k < steps; k += kChainWaves * kAhead) {
+        half8 h[kAhead][NB], l[kAhead][NB];
+#pragma unroll
+        for (uint32_t u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+                const uint8_t* src = x.frag(i, min(k + u * kChainWaves, steps - 1)) + lane * 16u;
+                h[u][i] = *reinterpret_cast<const half8*>(src);
+                l[u][i] = *reinterpret_cast<const half8*>(src + 1024);
+            }
+#pragma unroll
+        for (uint32_t u = 0; u < kAhead; ++u) {
+            if (k + u * kChainWaves >= steps) break;
+#pragma unroll
+            for (int i = 0; i < NB; ++i)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(h[u][i], l[u][j], acc[i][j], 0, 0, 0);
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[u][i], h[u][j], acc[i][j], 0, 0, 0);
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(h[u][i], h[u][j], acc[i][j], 0, 0, 0);
+                }
+        }
+    }
+    float4* sums = reinterpret_cast<float4*>(lds);  // [wave][block][4][lane]
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                sums[((wave * (NB * NB) + i * NB + j) * 4 + q) * 64 + lane] =
+                    make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+    __syncthreads();
+    constexpr int kUnits = NB * NB * 4, kEach = (kUnits + kChainWaves - 1) / kChainWaves;
+    float v[kEach][4];
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+        const uint32_t unit = wave * kEach + u;
+        v[u][0] = v[u][1] = v[u][2] = v[u][3] = 0.f;
+        if (unit < kUnits)
+            for (int w = 0; w < kChainWaves; ++w) {
+                const float4 f = sums[(w * kUnits + unit) * 64 + lane];
+                v[u][0] += f.x;
+                v[u][1] += f.y;
+                v[u][2] += f.z;
+                v[u][3] += f.w;
+            }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+        const uint32_t unit = wave * kEach + u, b = unit / 4;
+        if (unit >= kUnits) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[u][e] *= g.gram;
+        chain_write(Plane{lds, 2 * NB}, b / NB, b % NB, unit % 4, v[u], lane);
+    }
+    __syncthreads();
+}
+
+__global__ void __launch_bounds__(kChainThreads, 2) k_chain(ChainArgs g)
+{
+    extern __shared__ __align__(1024) uint8_t lds[];
+    const Common& c = g.c;
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    uint32_t at;
+    const Item it = c.items[find_item(c.starts + (size_t)kChain * c.count, c.count, blockIdx.x, &at)];
+    const uint32_t nb = (it.n + 31u) / 32u;
+    if (it.chain == 2) {
+        if (nb == 1) chain_gram<1>(g, it, lds, wave, lane);
+        else chain_gram<2>(g, it, lds, wave, lane);
+    } else {
+        const Plane from{c.ws + it.square + kA * it.square_bytes, it.nf};
+        for (uint32_t i = threadIdx.x; i < nb * nb * 2u * (kFragBytes / 16u); i += kChainThreads) {
+            const uint32_t frag = i / (kFragBytes / 16u), in = i % (kFragBytes / 16u);
+            *reinterpret_cast<uint4*>(lds + i * 16u) = *reinterpret_cast<const uint4*>(from.frag(frag / (2 * nb), frag % (2 * nb)) + in * 16u);
+        }
+        __syncthreads();
+    }
+    if (nb <= 2) chain_steps<1>(g, it, lds, nb, wave, lane);
+    else chain_steps<2>(g, it, lds, nb, wave, lane);
+}
+
+// ---- host ----
+// How a class of products is launched: tiles of 128 or 256, and the steps that a workgroup has at most.
+struct Share {
+    int size;
+    uint32_t len, workgroups;
+};
+struct Layout {
+    size_t items, starts, sums, arrivals, partial, total;
+    uint32_t count[kKinds], most;
+    Share share[kClasses];
+    bool fits;  // the counts are within 32 bits
+};
+
+uint32_t class_steps(const MatrixSpan& m, int cls)
+{
+    const uint32_t n = std::min(m.rows, m.cols), w = std::max(m.rows, m.cols);
+    return ((cls == kGrams ? w : n) + 15) / 16;
+}
+int chain_of(const MatrixSpan& m)
+{
+    const uint32_t n = std::min(m.rows, m.cols);
+    return n > kChainMost ? 0 : n <= kChainGram && class_steps(m, kGrams) <= kChainGramSteps ? 2 : 1;
+}
+uint64_t class_tiles(const MatrixSpan& m, int cls, int size)
+{
+    const uint64_t t = size ? 256 : 128, nt = (std::min(m.rows, m.cols) + t - 1) / t, mt = (std::max(m.rows, m.cols) + t - 1) / t;
+    const int chain = chain_of(m);
+    switch (cls) {
+        case kGrams: return chain == 2 ? 0 : nt * (nt + 1) / 2;
+        case kSingles: return chain ? 0 : nt * (nt + 1) / 2;
+        case kPairs: return chain ? 0 : nt * (nt + 1);
+        default: return nt * mt;
+    }
+}
+
+// What a launch takes, in us: a step of a tile, what a workgroup does before and behind its steps, and for a sliced tile, putting
+// a part down and taking one up.  By tile size.
+constexpr double kStepUs[2] = {0.37, 1.2}, kEndsUs[2] = {5.0, 12.0}, kPutUs[2] = {3.0, 9.0}, kTakeUs[2] = {2.0, 8.0};
+constexpr uint32_t kUnits = 256;  // compute units
+
+Share share_of(const MatrixSpan* m, int count, int cls, bool large)
+{
+    Share best{};
+    double least = 0.0;
+    uint32_t longest = 0;
+    for (int i = 0; i < count; ++i)
+        if (class_tiles(m[i], cls, 0)) longest = std::max(longest, class_steps(m[i], cls));
+    for (int size = 0; size < (large ? 2 : 1); ++size)
+        for (uint32_t slices = 1; slices <= kMostSlices && longest; ++slices) {
+            const uint32_t len = std::max(kLeastSteps, (longest + slices - 1) / slices);
+            double workgroups = 0, steps = 0, sliced = 0;
+            for (int i = 0; i < count; ++i) {
+                const double tiles = (double)class_tiles(m[i], cls, size);
+                const uint32_t per = class_steps(m[i], cls), s = (per + len - 1) / len;
+                workgroups += tiles * s;
+                steps += tiles * per;
+                if (s > 1) sliced += tiles * s;
+            }
+            // every compute unit has as many, or the work is even but for the last one's
+            const double one = std::min(len, longest) * kStepUs[size] + kEndsUs[size];
+            double us = std::min(std::ceil(workgroups / kUnits) * one, (steps * kStepUs[size] + workgroups * kEndsUs[size]) / kUnits + one);
+            if (sliced > 0) us += std::ceil(sliced / kUnits) * kPutUs[size] + slices * kTakeUs[size];
+            if (best.workgroups == 0 || us < least) {
+                least = us;
+                best = Share{size, len, (uint32_t)std::min(workgroups, 4e9)};
+            }
+            if (len == kLeastSteps) break;
+        }
+    return best;
+}
+
+// the matrices' places; each(i, item, units of the kinds before it)
 template <typename Each>
 Layout lay_out(const MatrixSpan* m, int count, Each&& each)
 {
     Layout l{};
-    // tiles of 256 where they are enough to fill the card
-    uint64_t large = 0;
+    uint64_t sum[kKinds] = {}, sums = 0;
+    bool large = false;
     for (int i = 0; i < count; ++i) {
-        const uint64_t n = std::min(m[i].rows, m[i].cols), w = std::max(m[i].rows, m[i].cols);
-        large += (n / 256) * (w / 256);
+        sums += std::min<uint32_t>(m[i].rows, kMostParts);  // at most
+        large = large || std::min(m[i].rows, m[i].cols) > 256;
     }
-    l.tile = large >= 256 ? Large::kTile : Small::kTile;
-    uint64_t sums = 0;
-    for (int i = 0; i < count; ++i) sums += std::min<uint32_t>(m[i].rows, 256);  // at most
+    const uint32_t room = large ? Large::kTile : Small::kTile;
+    for (int cls = 0; cls < kClasses; ++cls) l.share[cls] = share_of(m, count, cls, large);
     size_t off = 0;
     l.items = off;  off = align256(off + (size_t)count * sizeof(Item));
-    l.starts = off; off = align256(off + ((size_t)count + 1) * kKinds * 4);
+    l.starts = off; off = align256(off + (size_t)count * kKinds * 4);
     l.sums = off;   off = align256(off + sums * 8);
     for (int i = 0; i < count; ++i) {
         Item it{};
@@ -617,62 +885,80 @@ Layout lay_out(const MatrixSpan* m, int count, Each&& each)
         it.cols = m[i].cols;
         it.n = std::min(it.rows, it.cols);
         it.m = std::max(it.rows, it.cols);
-        it.nt = (it.n + l.tile - 1) / l.tile;
-        it.mt = (it.m + l.tile - 1) / l.tile;
+        const uint32_t np = (it.n + room - 1) / room * room, mp = (it.m + room - 1) / room * room;
+        it.nf = np / 16;
+        it.mf = mp / 16;
         it.gain = m[i].gain;
-        const size_t tile = (size_t)l.tile * l.tile * 4, x = (size_t)it.nt * it.mt * tile;
+        it.chain = (uint32_t)chain_of(m[i]);
+        const size_t x = (size_t)np * mp * 4;
         for (int k = 0; k < 2; ++k) {
             it.x[k] = off;  off += x;
             it.xt[k] = off; off += x;
         }
         it.square = off;
-        it.square_bytes = (size_t)it.nt * it.nt * tile;
+        it.square_bytes = (size_t)np * np * 4;
         off += kSquares * it.square_bytes;
         const size_t values = (size_t)it.n * it.m;
-        it.parts = (uint32_t)std::min<size_t>(std::min<size_t>(it.rows, 256), (values + 8191) / 8192);
-        const uint32_t tiles = it.nt * (it.nt + 1) / 2, per = l.tile / 64;
-        const uint32_t wgs[kKinds] = {it.parts, it.nt * per * it.mt * per, tiles, it.nt * it.mt, tiles * ((it.m + 15) / 16), tiles * ((it.n + 15) / 16), 0};
+        it.parts = (uint32_t)std::min<size_t>(std::min<size_t>(it.rows, kMostParts), (values + 8191) / 8192);
+        uint64_t units[kKinds] = {};
+        units[kNorm] = it.parts;
+        units[kConvert] = (uint64_t)((it.n + 63) / 64) * ((it.m + 63) / 64);
+        units[kChain] = it.chain != 0;
+        for (int cls = 0; cls < kClasses; ++cls) {
+            const Share& s = l.share[cls];
+            if (s.workgroups) units[kProducts + cls] = class_tiles(m[i], cls, s.size) * ((class_steps(m[i], cls) + s.len - 1) / s.len);
+        }
         each(i, it, l.count);
-        for (int k = 0; k < kKinds; ++k) l.count[k] += wgs[k];
+        for (int k = 0; k < kKinds; ++k) l.count[k] = (uint32_t)(sum[k] += units[k]);
     }
-    l.partial = align256(off);
-    const uint32_t sharing = std::min(sharing_slots(l.tile), (std::max(l.count[kGramSteps], 2 * l.count[kSquareSteps]) + kLeastShare - 1) / kLeastShare);
-    l.total = l.partial + (size_t)sharing * 2 * l.tile * l.tile * 4;
+    l.fits = true;
+    for (int k = 0; k < kKinds; ++k) l.fits = l.fits && sum[k] < (uint64_t)1 << 22;  // of 512 threads: within a launch's 2^32
+    size_t partial = 0;
+    for (int cls = 0; cls < kClasses; ++cls) {
+        const Share& s = l.share[cls];
+        bool sliced = false;
+        for (int i = 0; i < count; ++i) sliced = sliced || (class_tiles(m[i], cls, s.size) && class_steps(m[i], cls) > s.len);
+        if (!sliced) continue;
+        l.most = std::max(l.most, s.workgroups);
+        partial = std::max(partial, (size_t)s.workgroups * (s.size ? Large::kTileBytes : Small::kTileBytes));
+    }
+    l.arrivals = align256(off);
+    l.partial = align256(l.arrivals + (size_t)l.most * 4);
+    l.total = l.partial + partial;
     return l;
 }
 
-template <typename S, int WHAT>
-hipError_t launch_product(const char* name, const char* join, const ProductArgs& g, const Layout& places, hipStream_t s)
+hipError_t allow_lds(const void* kernel, std::atomic<bool> (&ready)[64], uint32_t bytes)
 {
-    static std::atomic<bool> ready[64] = {};  // by device
     int dev = 0;
     hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return e;
     if (dev < 0 || dev >= 64) return hipErrorInvalidDevice;
     if (!ready[dev]) {
-        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_product<S, WHAT>), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
-        if (e == hipSuccess && symmetric(WHAT))
-            e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_join<S, symmetric(WHAT) ? WHAT : kGram>), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
+        e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
         if (e != hipSuccess) return e;
         ready[dev] = true;
     }
-    ProductArgs a = g;
-    const uint32_t products = symmetric(WHAT) ? (uint32_t)g.products : 1u;
-    a.tiles = places.count[symmetric(WHAT) ? kTiles : kWide];
-    a.len = 0;
-    uint32_t wgs = a.tiles * products;
-    if constexpr (symmetric(WHAT)) {
-        const uint32_t total = places.count[WHAT == kGram ? kGramSteps : kSquareSteps];
-        const uint32_t slots = sharing_slots(S::kTile) / products;
-        if (a.tiles < slots) {
-            a.len = std::max(kLeastShare, (total + slots - 1) / slots);
-            wgs = (total + a.len - 1) / a.len * products;
-        }
-    }
-    FFTSP_LAUNCH(name, (k_product<S, WHAT>), dim3(wgs), dim3(S::kThreads), S::kLds, s, a);
-    if constexpr (symmetric(WHAT))
-        if (a.len) FFTSP_LAUNCH(join, (k_join<S, WHAT>), dim3(a.tiles * products), dim3(S::kThreads), S::kLds, s, a);
+    return hipSuccess;
+}
+
+template <typename S, int WHAT>
+hipError_t launch_shared(const char* name, const ProductArgs& g, uint32_t workgroups, hipStream_t s)
+{
+    static std::atomic<bool> ready[64] = {};  // by device
+    const hipError_t e = allow_lds(reinterpret_cast<const void*>(&k_product<S, WHAT>), ready, S::kLds);
+    if (e != hipSuccess) return e;
+    FFTSP_LAUNCH(name, (k_product<S, WHAT>), dim3(workgroups), dim3(S::kThreads), S::kLds, s, g);
     return hipGetLastError();
+}
+template <int WHAT>
+hipError_t launch_product(const char* name, ProductArgs g, const Layout& places, hipStream_t s)
+{
+    g.cls = WHAT == kGram ? kGrams : !symmetric(WHAT) ? kWides : WHAT == kTimes && g.products == 2 ? kPairs : kSingles;
+    const Share& share = places.share[g.cls];
+    if (share.workgroups == 0) return hipSuccess;
+    g.len = share.len;
+    return share.size ? launch_shared<Large, WHAT>(name, g, share.workgroups, s) : launch_shared<Small, WHAT>(name, g, share.workgroups, s);
 }
 
 // How many times a matrix of singular values up to `bound` its planes hold: a power of two that leaves a factor of two
@@ -684,32 +970,35 @@ float lift_for(double bound)
     return (float)std::ldexp(1.0, e);
 }
 
-template <typename S>
 hipError_t launch_steps(const Common& c, const OrthogonalArgs& a, const StepBounds& b, const Layout& places, hipStream_t s)
 {
     hipError_t e = hipSuccess;
     int step = 0;
     for (int phase = 0; phase < b.phases && e == hipSuccess; ++phase) {
         const float lx = lift_for(b.x[phase]);
+        ChainArgs chain{};
+        chain.c = c;
+        chain.phase = phase;
         ProductArgs g{};
         g.c = c;
         g.products = 1;
         g.phase = phase;
         g.out[0] = kA;
         float la = lift_for(b.a[step]), lq = 1.f;
-        g.scale[0] = la / (lx * lx);
-        e = launch_product<S, kGram>("orthogonal_gram", "orthogonal_gram_join", g, places, s);
+        chain.gram = g.scale[0] = la / (lx * lx);
+        e = launch_product<kGram>("orthogonal_gram", g, places, s);
         int q = kQ0;
         for (const int first = step; step < b.end[phase] && e == hipSuccess; ++step) {
+            ChainStep& st = chain.step[chain.steps++];
             const int p = step == first ? kQ0 : kP;
             const float lp = lift_for(p == kP ? b.p[step] : std::max(b.p[step], b.q[step]));
             g.products = 1;
-            g.ca = a.coefficients[3 * step] * lp;
-            g.cb = a.coefficients[3 * step + 1] * lp / la;
-            g.scale[0] = a.coefficients[3 * step + 2] * (lp / (la * la));
+            st.ca = g.ca = a.coefficients[3 * step] * lp;
+            st.cb = g.cb = a.coefficients[3 * step + 1] * lp / la;
+            st.poly = g.scale[0] = a.coefficients[3 * step + 2] * (lp / (la * la));
             g.left[0] = g.right[0] = kA;
             g.out[0] = p;
-            e = launch_product<S, kPoly>("orthogonal_poly", "orthogonal_poly_join", g, places, s);
+            e = launch_product<kPoly>("orthogonal_poly", g, places, s);
             if (e != hipSuccess) break;
             const bool again = step + 1 < b.end[phase];
             const float lt = lift_for(b.t[step]);
@@ -717,7 +1006,7 @@ hipError_t launch_steps(const Common& c, const OrthogonalArgs& a, const StepBoun
             if (again) {  // T = P A
                 g.left[k] = p;
                 g.right[k] = kA;
-                g.scale[k] = lt / (lp * la);
+                st.t = g.scale[k] = lt / (lp * la);
                 g.out[k++] = kT;
             }
             if (p == kP) {  // Q <- P Q
@@ -725,33 +1014,39 @@ hipError_t launch_steps(const Common& c, const OrthogonalArgs& a, const StepBoun
                 g.left[k] = kP;
                 g.right[k] = q;
                 q = q == kQ0 ? kQ1 : kQ0;
-                g.scale[k] = next / (lp * lq);
+                st.q = g.scale[k] = next / (lp * lq);
                 lq = next;
                 g.out[k++] = q;
             } else {
                 lq = lp;
             }
             g.products = k;
-            if (k) e = launch_product<S, kTimes>("orthogonal_times", "orthogonal_times_join", g, places, s);
+            if (k) e = launch_product<kTimes>("orthogonal_times", g, places, s);
             if (again && e == hipSuccess) {  // A <- T P
                 const float next = lift_for(b.a[step + 1]);
                 g.products = 1;
                 g.left[0] = kT;
                 g.right[0] = p;
-                g.scale[0] = next / (lt * lp);
+                st.a = g.scale[0] = next / (lt * lp);
                 la = next;
                 g.out[0] = kA;
-                e = launch_product<S, kTimes>("orthogonal_times", "orthogonal_times_join", g, places, s);
+                e = launch_product<kTimes>("orthogonal_times", g, places, s);
             }
+        }
+        if (e == hipSuccess && places.count[kChain]) {
+            static std::atomic<bool> ready[64] = {};
+            chain.q = q;
+            e = allow_lds(reinterpret_cast<const void*>(&k_chain), ready, kChainLds);
+            if (e == hipSuccess) FFTSP_LAUNCH("orthogonal_chain", k_chain, dim3(places.count[kChain]), dim3(kChainThreads), kChainLds, s, chain);
         }
         if (e != hipSuccess) break;
         g.left[0] = q;
         if (phase + 1 < b.phases) {
             g.scale[0] = lift_for(b.x[phase + 1]) / (lq * lx);
-            e = launch_product<S, kApply>("orthogonal_apply", "", g, places, s);
+            e = launch_product<kApply>("orthogonal_apply", g, places, s);
         } else {
             g.scale[0] = 1.f / (lq * lx);
-            e = launch_product<S, kLast>("orthogonal_last", "", g, places, s);
+            e = launch_product<kLast>("orthogonal_last", g, places, s);
         }
     }
     return e;
@@ -797,7 +1092,8 @@ bool step_bounds(const float* coefficients, int nsteps, StepBounds* b)
 
 size_t orthogonal_workspace(const MatrixSpan* m, int count)
 {
-    return count ? lay_out(m, count, [](int, const Item&, const uint32_t*) {}).total : 0;
+    const Layout l = lay_out(m, count, [](int, const Item&, const uint32_t*) {});
+    return count && l.fits ? l.total : 0;
 }
 
 hipError_t launch_orthogonal(const OrthogonalArgs& a, const MatrixSpan* m, int count, uint8_t* ws, hipStream_t s)
@@ -807,7 +1103,6 @@ hipError_t launch_orthogonal(const OrthogonalArgs& a, const MatrixSpan* m, int c
     uint32_t* starts = reinterpret_cast<uint32_t*>(ws + places.starts);
     ItemTable t{};
     t.total = (uint32_t)count;
-    for (int k = 0; k < kKinds; ++k) t.sum[k] = places.count[k];
     lay_out(m, count, [&](int i, const Item& it, const uint32_t* begun) {
         t.item[t.count] = it;
         for (int k = 0; k < kKinds; ++k) t.start[t.count][k] = begun[k];
@@ -836,14 +1131,15 @@ hipError_t launch_orthogonal(const OrthogonalArgs& a, const MatrixSpan* m, int c
     c.starts = starts;
     c.sums = reinterpret_cast<double*>(ws + places.sums);
     c.partial = ws + places.partial;
+    c.arrivals = reinterpret_cast<uint32_t*>(ws + places.arrivals);
     c.count = (uint32_t)count;
-    c.tile = places.tile;
+    c.most = places.most;
     c.lift = lift_for(a.bounds.x[0]);
     FFTSP_LAUNCH("orthogonal_norm", k_norm, dim3(places.count[kNorm]), dim3(256), 0, s, c);
     FFTSP_LAUNCH("orthogonal_convert", k_convert, dim3(places.count[kConvert]), dim3(256), 0, s, c);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    return places.tile == Large::kTile ? launch_steps<Large>(c, a, a.bounds, places, s) : launch_steps<Small>(c, a, a.bounds, places, s);
+    return launch_steps(c, a, a.bounds, places, s);
 }
 
 }  // namespace fftsp
