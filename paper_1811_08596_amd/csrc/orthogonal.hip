@@ -262,9 +262,9 @@ struct Shape {
     static constexpr uint32_t kTurn = 32 * 36 * 4;                      // a wave's part of LDS in the epilogue
     static constexpr uint32_t kLds = std::max(kStage * STAGES, kTurn * kWaves);
     static constexpr uint32_t kTileBytes = kTile * kTile * 4;
-    static_assert(kLeft == kRight && (kLeft + kRight) * 2 % kWaves == 0 && kPieces * (STAGES - 2) < 64, "");
+    static_assert(kLeft == kRight && (kLeft + kRight) * 2 % kWaves == 0 && kPieces * (STAGES - 2) < 64 && STAGES >= 3, "");
 };
-using Small = Shape<2, 2, 2, 2, 3>;  // 128 x 128, three workgroups to a compute unit
+using Small = Shape<2, 2, 2, 2, 5>;  // 128 x 128, two workgroups to a compute unit, which fill its LDS
 using Large = Shape<2, 4, 4, 2, 4>;  // 256 x 256, one
 
 template <int N>
@@ -283,10 +283,15 @@ struct Accumulators {
     float16v v[S::BM][S::BN];
 };
 
-// acc += sum over `steps` steps; left and right: fragments of the first row block and step, row_bytes to the next row block's
+// acc += sum over `steps` steps; left and right: fragments of the first row block and step, row_bytes to the next row block's.
+// A wave's fragments of a step are read from LDS while the step before is multiplied, and those reads and the next pieces from
+// memory are issued between the products, two products apart: behind the barrier they would hold up all waves at once (at
+// 4096 x 4096 x 4096 in tiles of 256 a step of 1536 cycles of matrix instructions took 2095 that way and takes 1724, in tiles
+// of 128 two workgroups' steps 1070 and now 806 of 768; the card then lowers its clock from 1.8 to 1.6 GHz, and 1.33 and 1.20
+// PFLOP/s become 1.38 and 1.22).  idle: a wave above the diagonal of a symmetric result, which only helps to bring the pieces.
 template <typename S>
 __device__ __forceinline__ void multiply(Accumulators<S>& acc, uint8_t* lds, const uint8_t* left, const uint8_t* right, uint64_t left_row,
-                                         uint64_t right_row, uint32_t steps, uint32_t wave, uint32_t lane)
+                                         uint64_t right_row, uint32_t steps, bool idle, uint32_t wave, uint32_t lane)
 {
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds + wave * (S::kPieces * 1024u);
     const uint8_t* src[S::kPieces];
@@ -295,47 +300,71 @@ __device__ __forceinline__ void multiply(Accumulators<S>& acc, uint8_t* lds, con
         const uint32_t p = wave * S::kPieces + q, rb = p >> 1;
         src[q] = (rb < S::kLeft ? left + rb * left_row : right + (rb - S::kLeft) * right_row) + (p & 1u) * 1024u;
     }
-    auto bring = [&](uint32_t slot) {
-#pragma unroll
-        for (int q = 0; q < S::kPieces; ++q) {
-            bring_piece(src[q], lane * 16u, lds0 + slot * S::kStage + q * 1024u);
-            src[q] += kFragBytes;
-        }
+    auto bring = [&](int q, uint32_t slot) {
+        bring_piece(src[q], lane * 16u, lds0 + slot * S::kStage + q * 1024u);
+        src[q] += kFragBytes;
     };
-    for (uint32_t s = 0; s + 1 < S::STAGES && s < steps; ++s) bring(s);
+    for (uint32_t s = 0; s + 1 < S::STAGES && s < steps; ++s)
+#pragma unroll
+        for (int q = 0; q < S::kPieces; ++q) bring(q, s);
     const uint32_t wi = (wave % S::WM) * S::BM, wj = (wave / S::WM) * S::BN;
+    constexpr int kReads = 2 * (S::BM + S::BN), kGroups = 3 * S::BM, kAside = S::kPieces + kReads;
+    // fragments of the wave's right blocks, then of its left ones, hi and lo
+    auto read = [&](half8 (&f)[kReads], uint32_t slot, int q) {
+        const uint32_t rb = q / 2 < S::BN ? S::kLeft + wj + q / 2 : wi + q / 2 - S::BN;
+        f[q] = *reinterpret_cast<const half8*>(lds + slot * S::kStage + rb * kFragBytes + (q & 1) * 1024u + lane * 16u);
+    };
     uint32_t slot = 0, next = S::STAGES - 1;
-    for (uint32_t k = 0; k < steps; ++k) {
-        // steps k + 1 .. k + STAGES - 2 may still be on their way
-        if (k + S::STAGES - 1 <= steps) arrived<(S::STAGES - 2) * S::kPieces>();
+    auto step = [&](uint32_t k, half8 (&now)[kReads], half8 (&then)[kReads]) {
+        // step k + 1 has to be there; steps k + 2 .. k + STAGES - 2 may still be on their way
+        if (k + S::STAGES - 1 <= steps) arrived<(S::STAGES - 3) * S::kPieces>();
         else arrived<0>();
-        if (k + S::STAGES - 1 < steps) bring(next);
-        const uint8_t* base = lds + slot * S::kStage + lane * 16u;
-        half8 lh[S::BM], ll[S::BM], rh[S::BN], rl[S::BN];
-#pragma unroll
-        for (int j = 0; j < S::BN; ++j) {
-            const uint8_t* p = base + (S::kLeft + wj + j) * kFragBytes;
-            rh[j] = *reinterpret_cast<const half8*>(p);
-            rl[j] = *reinterpret_cast<const half8*>(p + 1024);
-        }
-#pragma unroll
-        for (int i = 0; i < S::BM; ++i) {
-            const uint8_t* p = base + (wi + i) * kFragBytes;
-            lh[i] = *reinterpret_cast<const half8*>(p);
-            ll[i] = *reinterpret_cast<const half8*>(p + 1024);
-        }
-#pragma unroll
-        for (int i = 0; i < S::BM; ++i) {
-#pragma unroll
-            for (int j = 0; j < S::BN; ++j) acc.v[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lh[i], rl[j], acc.v[i][j], 0, 0, 0);
-#pragma unroll
-            for (int j = 0; j < S::BN; ++j) acc.v[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ll[i], rh[j], acc.v[i][j], 0, 0, 0);
-#pragma unroll
-            for (int j = 0; j < S::BN; ++j) acc.v[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lh[i], rh[j], acc.v[i][j], 0, 0, 0);
-        }
+        const bool more = k + S::STAGES - 1 < steps;
         slot = slot + 1 == S::STAGES ? 0 : slot + 1;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            const int t = g / S::BM, i = g % S::BM;  // hi lo, lo hi, hi hi
+#pragma unroll
+            for (int j = 0; j < S::BN; ++j)
+                acc.v[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now[2 * (S::BN + i) + (t == 1)], now[2 * j + (t == 0)], acc.v[i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int q = g * kAside / kGroups; q < (g + 1) * kAside / kGroups; ++q) {
+                const int piece = q * S::kPieces / kAside;  // pieces evenly among the reads
+                if ((q + 1) * S::kPieces / kAside > piece) {
+                    if (more) bring(piece, next);
+                } else {
+                    read(then, slot, q - piece);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
         next = next + 1 == S::STAGES ? 0 : next + 1;
+    };
+    if (S::STAGES - 1 <= steps) arrived<(S::STAGES - 2) * S::kPieces>();
+    else arrived<0>();
+    if (idle) {  // as many barriers as the others have
+        for (uint32_t k = 0; k < steps; ++k) {
+            if (k + S::STAGES - 1 <= steps) arrived<(S::STAGES - 3) * S::kPieces>();
+            else arrived<0>();
+            if (k + S::STAGES - 1 < steps)
+#pragma unroll
+                for (int q = 0; q < S::kPieces; ++q) bring(q, next);
+            next = next + 1 == S::STAGES ? 0 : next + 1;
+        }
+        arrived<0>();
+        return;
     }
+    half8 f[2][kReads];
+#pragma unroll
+    for (int q = 0; q < kReads; ++q) read(f[0], 0, q);
+    uint32_t k = 0;
+    for (; k + 2 <= steps; k += 2) {
+        step(k, f[0], f[1]);
+        step(k + 1, f[1], f[0]);
+    }
+    if (k < steps) step(k, f[0], f[1]);
     arrived<0>();  // LDS is free again
 }
 
@@ -353,6 +382,12 @@ struct ProductArgs {
     uint32_t len;                // steps that a workgroup has at most
 };
 
+// Of a tile on the diagonal: the wave's blocks are above it, or what is above the diagonal for them is left out
+template <typename S>
+__device__ __forceinline__ bool above(uint32_t wave) { return wave % S::WM < S::WM / 2 && wave / S::WM >= S::WN / 2; }
+template <typename S>
+__device__ __forceinline__ bool below(uint32_t wave) { return wave % S::WM >= S::WM / 2 && wave / S::WM < S::WN / 2; }
+
 // lane l has column l % 32 of a block and rows 8 (e / 4) + 4 (l / 32) + e % 4
 template <typename S, int WHAT>
 __device__ __forceinline__ void finish(const ProductArgs& g, const Item& it, int product, Accumulators<S>& acc, uint8_t* lds, uint32_t ti,
@@ -363,6 +398,7 @@ __device__ __forceinline__ void finish(const ProductArgs& g, const Item& it, int
     const uint32_t col = lane & 31u, half = lane >> 5;
     uint32_t* turn = reinterpret_cast<uint32_t*>(lds + wave * S::kTurn);
     constexpr uint32_t kBlocks = S::kTile / 32u;  // of a tile's side
+    if (symmetric(WHAT) && ti == tj && above<S>(wave)) return;
 #pragma unroll
     for (int i = 0; i < S::BM; ++i)
 #pragma unroll
@@ -434,7 +470,7 @@ __device__ __forceinline__ void finish(const ProductArgs& g, const Item& it, int
                 }
                 __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
                 __builtin_amdgcn_wave_barrier();
-                if (!symmetric(WHAT) || ti != tj) {  // the other orientation, hi and lo of a value in one word
+                if (!symmetric(WHAT) || ti != tj || below<S>(wave)) {  // the other orientation, hi and lo of a value in one word
 #pragma unroll
                     for (int kb = 0; kb < 2; ++kb) {
                         uint32_t w[8];
@@ -478,7 +514,8 @@ __device__ __forceinline__ void multiply_tile(const ProductArgs& g, const Item& 
     const uint64_t l = WHAT == kGram ? x : it.square + g.left[product] * it.square_bytes;
     const uint64_t r = WHAT == kGram ? x : WHAT == kApply || WHAT == kLast ? xt : it.square + g.right[product] * it.square_bytes;
     multiply<S>(acc, lds, c.ws + l + (uint64_t)ti * (S::kTile / 32u) * row + (uint64_t)first * kFragBytes,
-                c.ws + r + (uint64_t)tj * (S::kTile / 32u) * row + (uint64_t)first * kFragBytes, row, row, steps, wave, lane);
+                c.ws + r + (uint64_t)tj * (S::kTile / 32u) * row + (uint64_t)first * kFragBytes, row, row, steps,
+                symmetric(WHAT) && ti == tj && above<S>(wave), wave, lane);
 }
 
 // Memory that workgroups of one launch hand over: device-scope accesses, which pass the caches that are not shared
@@ -499,7 +536,6 @@ template <typename S, int WHAT>
 __global__ void __launch_bounds__(S::kThreads, 2) k_product(ProductArgs g)
 {
     extern __shared__ __align__(1024) uint8_t lds[];
-    __shared__ uint32_t before;
     const Common& c = g.c;
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // workgroups go round the eight XCDs: 32 tiles behind each other, which have operands in common, to each of them in turn
@@ -543,9 +579,11 @@ __global__ void __launch_bounds__(S::kThreads, 2) k_product(ProductArgs g)
                 for (int q = 0; q < 8; ++q) put(dst + ((i * S::BN + j) * 8 + q) * S::kThreads, acc.v[i][j][2 * q], acc.v[i][j][2 * q + 1]);
         arrived<0>();  // every wave's stores are where all can see them
         uint32_t* count = c.arrivals + wg0;
-        if (threadIdx.x == 0) before = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        uint32_t* before = reinterpret_cast<uint32_t*>(lds);
+        if (threadIdx.x == 0) *before = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __syncthreads();
-        if (__builtin_amdgcn_readfirstlane(before) + 1 < slices) return;
+        if (__builtin_amdgcn_readfirstlane(*before) + 1 < slices) return;
+        __syncthreads();  // LDS is free again
         if (threadIdx.x == 0) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         for (uint32_t s = 0; s < slices; ++s) {
             const uint64_t* src = part(s);
@@ -826,7 +864,7 @@ uint64_t class_tiles(const MatrixSpan& m, int cls, int size)
 
 // What a launch takes, in us: a step of a tile, what a workgroup does before and behind its steps, and for a sliced tile, putting
 // a part down and taking one up.  By tile size.
-constexpr double kStepUs[2] = {0.37, 1.2}, kEndsUs[2] = {5.0, 12.0}, kPutUs[2] = {3.0, 9.0}, kTakeUs[2] = {2.0, 8.0};
+constexpr double kStepUs[2] = {0.26, 1.09}, kEndsUs[2] = {5.0, 12.0}, kPutUs[2] = {3.0, 9.0}, kTakeUs[2] = {2.0, 8.0};
 constexpr uint32_t kUnits = 256;  // compute units
 
 Share share_of(const MatrixSpan* m, int count, int cls, bool large)
