@@ -128,19 +128,6 @@ __device__ __forceinline__ void store_some(T* p, uint32_t n, const float* v)
             if (e < n) p[e] = from_float<T>(v[e]);
     }
 }
-__device__ __forceinline__ void load_values(const void* p, int type, uint64_t i, uint32_t n, float* v)
-{
-    if (type == 0) load_some(static_cast<const float*>(p) + i, n, v);
-    else if (type == 1) load_some(static_cast<const Bf16*>(p) + i, n, v);
-    else load_some(static_cast<const F16*>(p) + i, n, v);
-}
-__device__ __forceinline__ void store_values(void* p, int type, uint64_t i, uint32_t n, const float* v)
-{
-    if (type == 0) store_some(static_cast<float*>(p) + i, n, v);
-    else if (type == 1) store_some(static_cast<Bf16*>(p) + i, n, v);
-    else store_some(static_cast<F16*>(p) + i, n, v);
-}
-
 struct Common {
     const void* in;
     const float* momentum;
@@ -388,111 +375,167 @@ __device__ __forceinline__ bool above(uint32_t wave) { return wave % S::WM < S::
 template <typename S>
 __device__ __forceinline__ bool below(uint32_t wave) { return wave % S::WM >= S::WM / 2 && wave / S::WM < S::WN / 2; }
 
+// The last product's tile to the caller's array, through LDS, so that lanes go along its rows.  The weights of the next blocks
+// are on their way while these are written.
+template <typename S, typename T>
+__device__ __forceinline__ void finish_last(const ProductArgs& g, const Item& it, Accumulators<S>& acc, uint8_t* lds, uint32_t ti, uint32_t tj,
+                                            uint32_t wave, uint32_t lane)
+{
+    const Common& c = g.c;
+    const uint32_t wi = (wave % S::WM) * S::BM, wj = (wave / S::WM) * S::BN;
+    const uint32_t col = lane & 31u, half = lane >> 5;
+    float* turn = reinterpret_cast<float*>(lds + wave * S::kTurn);
+    constexpr uint32_t kBlocks = S::kTile / 32u;  // of a tile's side
+    const bool t = tall(it), step = c.step != 0;
+    const float scale = it.gain * g.scale[0];
+    const T* weights = static_cast<const T*>(c.weights);
+    T* out = static_cast<T*>(c.out);
+    // a lane's four values of row 8 q + lane / 8 of a block: the element, and how many of them there are
+    auto place = [&](int i, int j, int q, uint64_t* el) {
+        const uint32_t bi = ti * kBlocks + wi + i, bj = tj * kBlocks + wj + j;
+        const uint32_t row = (t ? bj : bi) * 32u + q * 8u + (lane >> 3), first = (t ? bi : bj) * 32u + (lane & 7u) * 4u;
+        *el = it.at + (uint64_t)row * it.stride + first;
+        return row < it.rows && first < it.cols ? min(4u, it.cols - first) : 0u;
+    };
+    float w[2][S::BN][4][4];
+    auto fetch = [&](float (&v)[S::BN][4][4], int i) {
+#pragma unroll
+        for (int j = 0; j < S::BN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                uint64_t el;
+                const uint32_t n = place(i, j, q, &el);
+                if (n) load_some<T>(weights + el, n, v[j][q]);
+            }
+    };
+    if (step) fetch(w[0], 0);
+#pragma unroll
+    for (int i = 0; i < S::BM; ++i) {
+        if (step && i + 1 < S::BM) fetch(w[(i + 1) & 1], i + 1);
+#pragma unroll
+        for (int j = 0; j < S::BN; ++j) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const uint32_t r = 8 * (e / 4) + 4 * half + e % 4;
+                turn[t ? col * 36u + r : r * 36u + col] = acc.v[i][j][e] * scale;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                uint64_t el;
+                const uint32_t n = place(i, j, q, &el);
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = turn[(q * 8u + (lane >> 3)) * 36u + (lane & 7u) * 4u + e];
+                if (n) {
+                    if (step)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = fmaf(-c.lr, v[e], c.decay * w[i & 1][j][q][e]);
+                    store_some<T>(out + el, n, v);
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+}
+
+// Any other product's tile to fragments, in both orientations.
 // lane l has column l % 32 of a block and rows 8 (e / 4) + 4 (l / 32) + e % 4
 template <typename S, int WHAT>
 __device__ __forceinline__ void finish(const ProductArgs& g, const Item& it, int product, Accumulators<S>& acc, uint8_t* lds, uint32_t ti,
                                        uint32_t tj, uint32_t wave, uint32_t lane)
 {
     const Common& c = g.c;
+    if constexpr (WHAT == kLast) {
+        if (c.out_type == 0) finish_last<S, float>(g, it, acc, lds, ti, tj, wave, lane);
+        else if (c.out_type == 1) finish_last<S, Bf16>(g, it, acc, lds, ti, tj, wave, lane);
+        else finish_last<S, F16>(g, it, acc, lds, ti, tj, wave, lane);
+        return;
+    }
     const uint32_t wi = (wave % S::WM) * S::BM, wj = (wave / S::WM) * S::BN;
     const uint32_t col = lane & 31u, half = lane >> 5;
     uint32_t* turn = reinterpret_cast<uint32_t*>(lds + wave * S::kTurn);
     constexpr uint32_t kBlocks = S::kTile / 32u;  // of a tile's side
     if (symmetric(WHAT) && ti == tj && above<S>(wave)) return;
+    const int out = g.out[product];
+    uint8_t* direct = c.ws + (symmetric(WHAT) ? it.square + out * it.square_bytes : by_columns(it, g.phase + 1));  // rows: C's columns
+    uint8_t* turned = c.ws + (symmetric(WHAT) ? it.square + out * it.square_bytes : by_rows(it, g.phase + 1));
+    const uint8_t* a = c.ws + it.square + kA * it.square_bytes;
+    const uint32_t direct_row = it.nf, turned_row = symmetric(WHAT) ? it.nf : it.mf;
+    // four values of a lane in the fragments whose rows are C's columns
+    auto place = [&](int i, int j, int q) {
+        const uint32_t bi = ti * kBlocks + wi + i, bj = tj * kBlocks + wj + j;
+        return ((uint64_t)bj * direct_row + bi * 2u + q / 2) * kFragBytes + (col + 32u * (q & 1)) * 16u + half * 8u;
+    };
+    half4 ah[2][S::BN][4], al[2][S::BN][4];  // kPoly: A there, the next blocks' on their way while these are written
+    auto fetch = [&](int b, int i) {
 #pragma unroll
-    for (int i = 0; i < S::BM; ++i)
+        for (int j = 0; j < S::BN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint8_t* src = a + place(i, j, q);
+                ah[b][j][q] = *reinterpret_cast<const half4*>(src);
+                al[b][j][q] = *reinterpret_cast<const half4*>(src + 1024);
+            }
+    };
+    if constexpr (WHAT == kPoly) fetch(0, 0);
+#pragma unroll
+    for (int i = 0; i < S::BM; ++i) {
+        if constexpr (WHAT == kPoly)
+            if (i + 1 < S::BM) fetch((i + 1) & 1, i + 1);
 #pragma unroll
         for (int j = 0; j < S::BN; ++j) {
             const uint32_t bi = ti * kBlocks + wi + i, bj = tj * kBlocks + wj + j;
-            if constexpr (WHAT == kLast) {
-                // through LDS, so that lanes go along the caller's rows
-                const bool t = tall(it);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const uint32_t r = 8 * (e / 4) + 4 * half + e % 4;
-                    turn[t ? col * 36u + r : r * 36u + col] = __float_as_uint(it.gain * (acc.v[i][j][e] * g.scale[0]));
-                }
-                __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-                __builtin_amdgcn_wave_barrier();
+            for (int q = 0; q < 4; ++q) {
+                half4 hi, lo;
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const uint32_t slow = q * 8u + (lane >> 3), fast = (lane & 7u) * 4u;
-                    const uint32_t row = (t ? bj : bi) * 32u + slow, first = (t ? bi : bj) * 32u + fast;
-                    float v[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(turn[slow * 36u + fast + e]);
-                    if (row < it.rows && first < it.cols) {
-                        const uint64_t el = it.at + (uint64_t)row * it.stride + first;
-                        const uint32_t there = min(4u, it.cols - first);
-                        if (c.step) {
-                            float w[4];
-                            load_values(c.weights, c.out_type, el, there, w);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) v[e] = fmaf(-c.lr, v[e], c.decay * w[e]);
-                        }
-                        store_values(c.out, c.out_type, el, there, v);
-                    }
-                }
-            } else {
-                const int out = g.out[product];
-                uint8_t* direct = c.ws + (symmetric(WHAT) ? it.square + out * it.square_bytes : by_columns(it, g.phase + 1));  // rows: C's columns
-                uint8_t* turned = c.ws + (symmetric(WHAT) ? it.square + out * it.square_bytes : by_rows(it, g.phase + 1));
-                const uint32_t direct_row = it.nf, turned_row = symmetric(WHAT) ? it.nf : it.mf;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    half4 hi, lo, ah, al;
-                    const uint64_t frag = (uint64_t)bj * direct_row + bi * 2u + q / 2;
-                    const uint32_t in_frag = (col + 32u * (q & 1)) * 16u + half * 8u;
+                for (int e = 0; e < 4; ++e) {
+                    float v = acc.v[i][j][q * 4 + e] * g.scale[product];
                     if constexpr (WHAT == kPoly) {
-                        const uint8_t* src = c.ws + it.square + kA * it.square_bytes + frag * kFragBytes + in_frag;
-                        ah = *reinterpret_cast<const half4*>(src);
-                        al = *reinterpret_cast<const half4*>(src + 1024);
+                        v = fmaf(g.cb, (float)ah[i & 1][j][q][e] + (float)al[i & 1][j][q][e], v);
+                        if (bi == bj && col == 8u * q + 4u * half + e) v += g.ca;
                     }
+                    _Float16 h, l;
+                    split(v, &h, &l);
+                    hi[e] = h;
+                    lo[e] = l;
+                    uint16_t hb, lb;
+                    __builtin_memcpy(&hb, &h, 2);
+                    __builtin_memcpy(&lb, &l, 2);
+                    turn[(8 * q + 4 * half + e) * 36 + col] = (uint32_t)hb | (uint32_t)lb << 16;
+                }
+                uint8_t* dst = direct + place(i, j, q);
+                *reinterpret_cast<half4*>(dst) = hi;
+                *reinterpret_cast<half4*>(dst + 1024) = lo;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            if (!symmetric(WHAT) || ti != tj || below<S>(wave)) {  // the other orientation, hi and lo of a value in one word
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    uint32_t w[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) w[e] = turn[col * 36 + kb * 16 + half * 8 + e];
+                    uint4 hi, lo;
+                    uint32_t* ph = reinterpret_cast<uint32_t*>(&hi);
+                    uint32_t* pl = reinterpret_cast<uint32_t*>(&lo);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        float v = acc.v[i][j][q * 4 + e] * g.scale[product];
-                        if constexpr (WHAT == kPoly) {
-                            v = fmaf(g.cb, (float)ah[e] + (float)al[e], v);
-                            if (bi == bj && col == 8u * q + 4u * half + e) v += g.ca;
-                        }
-                        _Float16 h, l;
-                        split(v, &h, &l);
-                        hi[e] = h;
-                        lo[e] = l;
-                        uint16_t hb, lb;
-                        __builtin_memcpy(&hb, &h, 2);
-                        __builtin_memcpy(&lb, &l, 2);
-                        turn[(8 * q + 4 * half + e) * 36 + col] = (uint32_t)hb | (uint32_t)lb << 16;
+                        ph[e] = (w[2 * e] & 0xFFFFu) | w[2 * e + 1] << 16;
+                        pl[e] = w[2 * e] >> 16 | (w[2 * e + 1] & 0xFFFF0000u);
                     }
-                    uint8_t* dst = direct + frag * kFragBytes + in_frag;
-                    *reinterpret_cast<half4*>(dst) = hi;
-                    *reinterpret_cast<half4*>(dst + 1024) = lo;
-                }
-                __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-                if (!symmetric(WHAT) || ti != tj || below<S>(wave)) {  // the other orientation, hi and lo of a value in one word
-#pragma unroll
-                    for (int kb = 0; kb < 2; ++kb) {
-                        uint32_t w[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) w[e] = turn[col * 36 + kb * 16 + half * 8 + e];
-                        uint4 hi, lo;
-                        uint32_t* ph = reinterpret_cast<uint32_t*>(&hi);
-                        uint32_t* pl = reinterpret_cast<uint32_t*>(&lo);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            ph[e] = (w[2 * e] & 0xFFFFu) | w[2 * e + 1] << 16;
-                            pl[e] = w[2 * e] >> 16 | (w[2 * e + 1] & 0xFFFF0000u);
-                        }
-                        uint8_t* dst = turned + ((uint64_t)bi * turned_row + bj * 2u + kb) * kFragBytes + lane * 16u;
-                        *reinterpret_cast<uint4*>(dst) = hi;
-                        *reinterpret_cast<uint4*>(dst + 1024) = lo;
-                    }
+                    uint8_t* dst = turned + ((uint64_t)bi * turned_row + bj * 2u + kb) * kFragBytes + lane * 16u;
+                    *reinterpret_cast<uint4*>(dst) = hi;
+                    *reinterpret_cast<uint4*>(dst + 1024) = lo;
                 }
             }
             __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
             __builtin_amdgcn_wave_barrier();
         }
+    }
 }
 
 __device__ __forceinline__ uint32_t steps_of(const Item& it, int what) { return ((what == kGram ? it.m : it.n) + 15u) / 16u; }
