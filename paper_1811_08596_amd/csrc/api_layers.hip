@@ -103,7 +103,8 @@ int check_steps(OrthogonalArgs* a, const float* coefficients, int nsteps, float 
     if (a->nsteps < 1 || a->nsteps > FFTSP_MAX_STEPS) return FFTSP_EINVAL;
     for (int i = 0; i < 3 * a->nsteps; ++i)
         if (!std::isfinite(a->coefficients[i])) return FFTSP_EINVAL;
-    return step_bounds(a->coefficients, a->nsteps, &a->bounds) ? FFTSP_OK : FFTSP_EUNSUPPORTED;
+    StepBounds bounds;
+    return step_bounds(a->coefficients, a->nsteps, kPhaseMost, &bounds) ? FFTSP_OK : FFTSP_EUNSUPPORTED;
 }
 
 int run_orthogonal(const OrthogonalArgs& a, const fftsp_matrix* m, int count, void* ws, size_t ws_bytes, fftsp_stream_t stream)

@@ -82,7 +82,7 @@ size_t embedding_gradient_workspace(size_t rows, uint32_t width, size_t ntokens)
 hipError_t launch_embedding_gradient(const EmbeddingArgs& a, uint8_t* ws, hipStream_t s);
 
 // orthogonal.hip
-constexpr int kPhaseSteps = 3;        // steps that are taken on n x n matrices before X is
+constexpr int kPhaseMost = 3, kPhaseMost32 = 2;  // steps that are taken on n x n matrices before X is, for results in 16 and in 32 bits
 constexpr int kMostSteps = 16;
 constexpr double kMostBound = 4096.0;  // of a matrix's singular values anywhere in the iteration
 struct StepBounds {                   // largest singular values: X before each phase; A, P, P A, and the phase's product of P, by step
@@ -90,7 +90,7 @@ struct StepBounds {                   // largest singular values: X before each 
     double x[kMostSteps], a[kMostSteps], p[kMostSteps], t[kMostSteps], q[kMostSteps];
 };
 // false: some are larger than kMostBound
-bool step_bounds(const float* coefficients, int nsteps, StepBounds* b);
+bool step_bounds(const float* coefficients, int nsteps, int phase_steps, StepBounds* b);
 
 struct OrthogonalArgs {
     const void* in;        // the matrices, or the gradient
@@ -106,7 +106,6 @@ struct OrthogonalArgs {
     float eps;
     const float* coefficients;  // host, 3 per step
     int nsteps;
-    StepBounds bounds;
 };
 struct MatrixSpan {  // fftsp_matrix
     uint64_t offset, stride;

@@ -2,12 +2,13 @@
 //
 //   X = U / (|U|_F + eps), n x m with n <= m;   per step  A = X X^T,  P = a I + b A + c A A,  X <- P X;   out = gain X
 //
-// The products carry the time.  All matrices of a phase of up to three steps are polynomials of the phase's first A, so
+// The products carry the time.  All matrices of a phase of a few steps are polynomials of the phase's first A, so
 // they commute, and the steps can be taken on n x n matrices alone: Q <- P Q, A <- P A P, and X <- Q X at the phase's end.
 // That is n^2 m for A and 2 n^2 m for Q X once a phase instead of once a step, and four symmetric n x n products (n^3
-// each: only tiles on and under the diagonal are computed, and written twice) a step instead of one.  A phase ends after
-// three steps because A has an absolute error of 2^-24 of its largest eigenvalue, which the small eigenvalues' growth by
-// a^2 a step turns into a relative one: 3.4445^4 2^-24 = 1e-5 after three steps, 1e-3 after five.
+// each: only tiles on and under the diagonal are computed, and written twice) a step instead of one.  A has an absolute error
+// of 2^-24 of its largest eigenvalue, which the small eigenvalues' growth by a^2 a step turns into a relative one: 1e-6 after
+// two steps, 3.4445^4 2^-24 = 1e-5 after three, 1e-3 after five.  So a phase has up to two steps where the result is stored in
+// 32 bits, up to three where it is rounded to 16.
 //
 // Products run on binary16 matrix instructions whose inputs carry a binary32 number in two planes: 2^e v = hi + lo, each
 // rounded to nearest (v is then 2^-24 v off, or 2^-(25 + e) where v is small), and x y = hi hi + hi lo + lo hi summed in
@@ -656,7 +657,7 @@ struct ChainStep {
 };
 struct ChainArgs {
     Common c;
-    ChainStep step[kPhaseSteps];
+    ChainStep step[kPhaseMost];
     int steps, phase, q;  // q: where the apply looks for Q
     float gram;
 };
@@ -875,11 +876,13 @@ __global__ void __launch_bounds__(kChainThreads, 2) k_chain(ChainArgs g)
 struct Share {
     int size;
     uint32_t len, workgroups;
+    double us;  // what it is thought to take
 };
 struct Layout {
     size_t items, starts, sums, arrivals, partial, total;
     uint32_t count[kKinds], most;
     Share share[kClasses];
+    int phase_steps;
     bool fits;  // the counts are within 32 bits
 };
 
@@ -909,6 +912,7 @@ uint64_t class_tiles(const MatrixSpan& m, int cls, int size)
 // a part down and taking one up.  By tile size.
 constexpr double kStepUs[2] = {0.26, 1.09}, kEndsUs[2] = {5.0, 12.0}, kPutUs[2] = {3.0, 9.0}, kTakeUs[2] = {2.0, 8.0};
 constexpr uint32_t kUnits = 256;  // compute units
+constexpr double kChainUs = 6.0, kChainStepUs = 5.0;
 
 Share share_of(const MatrixSpan* m, int count, int cls, bool large)
 {
@@ -934,16 +938,41 @@ Share share_of(const MatrixSpan* m, int count, int cls, bool large)
             if (sliced > 0) us += std::ceil(sliced / kUnits) * kPutUs[size] + slices * kTakeUs[size];
             if (best.workgroups == 0 || us < least) {
                 least = us;
-                best = Share{size, len, (uint32_t)std::min(workgroups, 4e9)};
+                best = Share{size, len, (uint32_t)std::min(workgroups, 4e9), us};
             }
             if (len == kLeastSteps) break;
         }
     return best;
 }
 
+// Steps of a phase: one (X X^T, P, P X) or several, whichever is thought to take less.  Matrices that are about square have as
+// much work either way, and then one has fewer launches; wide ones gain from several.
+int phase_steps_of(const Share* share, bool chains, int nsteps, int most)
+{
+    int best = 1;
+    double least = 0.0;
+    for (int length = 1; length <= most; ++length) {
+        const int phases = (nsteps + length - 1) / length;
+        double us = phases * (share[kGrams].us + share[kWides].us);
+        for (int p = 0, step = 0; p < phases; ++p) {
+            const int steps = (nsteps * (p + 1) + phases - 1) / phases - step;
+            step += steps;
+            us += steps * share[kSingles].us;  // P
+            // the first step's P A, the last one's P Q and every other's two at once; A
+            if (steps > 1) us += (steps + 1) * share[kSingles].us + (steps - 2) * share[kPairs].us;
+            if (chains) us += kChainUs + steps * kChainStepUs;
+        }
+        if (length == 1 || us < least) {
+            least = us;
+            best = length;
+        }
+    }
+    return best;
+}
+
 // the matrices' places; each(i, item, units of the kinds before it)
 template <typename Each>
-Layout lay_out(const MatrixSpan* m, int count, Each&& each)
+Layout lay_out(const MatrixSpan* m, int count, int nsteps, int most_phase, Each&& each)
 {
     Layout l{};
     uint64_t sum[kKinds] = {}, sums = 0;
@@ -1003,6 +1032,7 @@ Layout lay_out(const MatrixSpan* m, int count, Each&& each)
         l.most = std::max(l.most, s.workgroups);
         partial = std::max(partial, (size_t)s.workgroups * (s.size ? Large::kTileBytes : Small::kTileBytes));
     }
+    l.phase_steps = phase_steps_of(l.share, l.count[kChain] != 0, nsteps, most_phase);
     l.arrivals = align256(off);
     l.partial = align256(l.arrivals + (size_t)l.most * 4);
     l.total = l.partial + partial;
@@ -1136,12 +1166,12 @@ hipError_t launch_steps(const Common& c, const OrthogonalArgs& a, const StepBoun
 }  // namespace
 
 // The singular values of X, A, P, T = P A and the phase's Q, from a grid over those that X can begin with.
-bool step_bounds(const float* coefficients, int nsteps, StepBounds* b)
+bool step_bounds(const float* coefficients, int nsteps, int phase_steps, StepBounds* b)
 {
     constexpr int kGrid = 256;
     double x[kGrid + 1], q[kGrid + 1];
     for (int i = 0; i <= kGrid; ++i) x[i] = (double)i / kGrid;
-    b->phases = (nsteps + kPhaseSteps - 1) / kPhaseSteps;
+    b->phases = (nsteps + phase_steps - 1) / phase_steps;
     int step = 0;
     for (int phase = 0; phase < b->phases; ++phase) {
         b->end[phase] = (nsteps * (phase + 1) + b->phases - 1) / b->phases;
@@ -1173,18 +1203,21 @@ bool step_bounds(const float* coefficients, int nsteps, StepBounds* b)
 
 size_t orthogonal_workspace(const MatrixSpan* m, int count)
 {
-    const Layout l = lay_out(m, count, [](int, const Item&, const uint32_t*) {});
+    const Layout l = lay_out(m, count, 1, 1, [](int, const Item&, const uint32_t*) {});
     return count && l.fits ? l.total : 0;
 }
 
 hipError_t launch_orthogonal(const OrthogonalArgs& a, const MatrixSpan* m, int count, uint8_t* ws, hipStream_t s)
 {
-    const Layout places = lay_out(m, count, [](int, const Item&, const uint32_t*) {});
+    const int most = a.out_type == 0 ? kPhaseMost32 : kPhaseMost;
+    const Layout places = lay_out(m, count, a.nsteps, most, [](int, const Item&, const uint32_t*) {});
+    StepBounds bounds;
+    if (!step_bounds(a.coefficients, a.nsteps, places.phase_steps, &bounds)) return hipErrorInvalidValue;
     Item* items = reinterpret_cast<Item*>(ws + places.items);
     uint32_t* starts = reinterpret_cast<uint32_t*>(ws + places.starts);
     ItemTable t{};
     t.total = (uint32_t)count;
-    lay_out(m, count, [&](int i, const Item& it, const uint32_t* begun) {
+    lay_out(m, count, a.nsteps, most, [&](int i, const Item& it, const uint32_t* begun) {
         t.item[t.count] = it;
         for (int k = 0; k < kKinds; ++k) t.start[t.count][k] = begun[k];
         if (++t.count == kItemsPerLaunch || i + 1 == count) {
@@ -1215,12 +1248,12 @@ hipError_t launch_orthogonal(const OrthogonalArgs& a, const MatrixSpan* m, int c
     c.arrivals = reinterpret_cast<uint32_t*>(ws + places.arrivals);
     c.count = (uint32_t)count;
     c.most = places.most;
-    c.lift = lift_for(a.bounds.x[0]);
+    c.lift = lift_for(bounds.x[0]);
     FFTSP_LAUNCH("orthogonal_norm", k_norm, dim3(places.count[kNorm]), dim3(256), 0, s, c);
     FFTSP_LAUNCH("orthogonal_convert", k_convert, dim3(places.count[kConvert]), dim3(256), 0, s, c);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    return launch_steps(c, a, a.bounds, places, s);
+    return launch_steps(c, a, bounds, places, s);
 }
 
 }  // namespace fftsp
