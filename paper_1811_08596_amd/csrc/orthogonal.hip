@@ -147,26 +147,50 @@ struct Common {
 };
 
 // ---- momentum and |U|_F^2 ----
+// A workgroup has pieces of kPiece values of a row, or of the whole matrix where its rows follow each other, in turn.
+constexpr uint32_t kPiece = 1024;
+template <typename T, bool STEP>
+__device__ __forceinline__ double norm_part(const Common& c, const Item& it, uint32_t part)
+{
+    const bool flat = it.stride == it.cols;
+    const uint64_t rows = flat ? 1 : it.rows, cols = flat ? (uint64_t)it.rows * it.cols : it.cols;
+    const uint32_t across = (uint32_t)((cols + kPiece - 1) / kPiece);
+    const uint64_t pieces = rows * across;
+    double s = 0.0;
+    for (uint64_t p = part; p < pieces; p += it.parts) {
+        const uint64_t row = flat ? 0 : p / across, first = (p - row * across) * kPiece + threadIdx.x * 4u;
+        if (first >= cols) continue;
+        const uint64_t at = it.at + row * it.stride + first;
+        const uint32_t n = (uint32_t)min((uint64_t)4, cols - first);
+        float u[4];
+        load_some<T>(static_cast<const T*>(c.in) + at, n, u);
+        if (STEP) {
+            float m[4];
+            load_some<float>(c.momentum + at, n, m);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m[e] = fmaf(c.beta, m[e], u[e]);
+            store_some<float>(c.momentum_out + at, n, m);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) u[e] = c.nesterov ? fmaf(c.beta, m[e], u[e]) : m[e];
+        }
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e)
+            if (e < n) s += (double)u[e] * (double)u[e];
+    }
+    return s;
+}
+template <typename T>
+__device__ __forceinline__ double norm_of_type(const Common& c, const Item& it, uint32_t part)
+{
+    return c.step ? norm_part<T, true>(c, it, part) : norm_part<T, false>(c, it, part);
+}
 __global__ void __launch_bounds__(256) k_norm(Common c)
 {
     __shared__ double sums[4];
     uint32_t part;
     const Item it = c.items[find_item(c.starts + (size_t)kNorm * c.count, c.count, blockIdx.x, &part)];
     for (uint32_t i = blockIdx.x * 256u + threadIdx.x; i < c.most; i += gridDim.x * 256u) c.arrivals[i] = 0;
-    double s = 0.0;
-    // a workgroup has whole rows in turn
-    for (uint32_t r = part; r < it.rows; r += it.parts) {
-        const uint64_t row = it.at + (uint64_t)r * it.stride;
-        for (uint32_t j = threadIdx.x; j < it.cols; j += 256) {
-            float u = load_value(c.in, c.in_type, row + j);
-            if (c.step) {
-                const float m = fmaf(c.beta, c.momentum[row + j], u);
-                c.momentum_out[row + j] = m;
-                u = c.nesterov ? fmaf(c.beta, m, u) : m;
-            }
-            s += (double)u * (double)u;
-        }
-    }
+    double s = c.in_type == 0 ? norm_of_type<float>(c, it, part) : c.in_type == 1 ? norm_of_type<Bf16>(c, it, part) : norm_of_type<F16>(c, it, part);
     for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
     if ((threadIdx.x & 63u) == 0) sums[threadIdx.x >> 6] = s;
     __syncthreads();
@@ -252,8 +276,11 @@ struct Shape {
     static constexpr uint32_t kTileBytes = kTile * kTile * 4;
     static_assert(kLeft == kRight && (kLeft + kRight) * 2 % kWaves == 0 && kPieces * (STAGES - 2) < 64 && STAGES >= 3, "");
 };
+using Least = Shape<2, 2, 1, 1, 8>;  // 64 x 64
 using Small = Shape<2, 2, 2, 2, 5>;  // 128 x 128, two workgroups to a compute unit, which fill its LDS
 using Large = Shape<2, 4, 4, 2, 4>;  // 256 x 256, one
+constexpr int kSizes = 3;
+constexpr uint32_t kTileOf[kSizes] = {Least::kTile, Small::kTile, Large::kTile}, kTileBytesOf[kSizes] = {Least::kTileBytes, Small::kTileBytes, Large::kTileBytes};
 
 template <int N>
 __device__ __forceinline__ void arrived()  // all but the wave's last N pieces; then everybody's
@@ -872,7 +899,7 @@ __global__ void __launch_bounds__(kChainThreads, 2) k_chain(ChainArgs g)
 }
 
 // ---- host ----
-// How a class of products is launched: tiles of 128 or 256, and the steps that a workgroup has at most.
+// How a class of products is launched: the tiles' size, and the steps that a workgroup has at most.
 struct Share {
     int size;
     uint32_t len, workgroups;
@@ -886,20 +913,28 @@ struct Layout {
     bool fits;  // the counts are within 32 bits
 };
 
+// workgroups that sum a matrix's squares: up to kMostParts, with two pieces each or more
+uint32_t norm_parts(const MatrixSpan& m)
+{
+    const uint64_t pieces = m.stride == m.cols ? ((uint64_t)m.rows * m.cols + kPiece - 1) / kPiece : (uint64_t)m.rows * ((m.cols + kPiece - 1) / kPiece);
+    return (uint32_t)std::min<uint64_t>(kMostParts, (pieces + 1) / 2);
+}
 uint32_t class_steps(const MatrixSpan& m, int cls)
 {
     const uint32_t n = std::min(m.rows, m.cols), w = std::max(m.rows, m.cols);
     return ((cls == kGrams ? w : n) + 15) / 16;
 }
-int chain_of(const MatrixSpan& m)
+// chains: every matrix of the list is short enough.  Beside longer ones, whose launches there are anyway, the short ones' tiles
+// cost nothing, and their chains would hold up the others.
+int chain_of(const MatrixSpan& m, bool chains)
 {
-    const uint32_t n = std::min(m.rows, m.cols);
-    return n > kChainMost ? 0 : n <= kChainGram && class_steps(m, kGrams) <= kChainGramSteps ? 2 : 1;
+    if (!chains) return 0;
+    return std::min(m.rows, m.cols) <= kChainGram && class_steps(m, kGrams) <= kChainGramSteps ? 2 : 1;
 }
-uint64_t class_tiles(const MatrixSpan& m, int cls, int size)
+uint64_t class_tiles(const MatrixSpan& m, bool chains, int cls, int size)
 {
-    const uint64_t t = size ? 256 : 128, nt = (std::min(m.rows, m.cols) + t - 1) / t, mt = (std::max(m.rows, m.cols) + t - 1) / t;
-    const int chain = chain_of(m);
+    const uint64_t t = kTileOf[size], nt = (std::min(m.rows, m.cols) + t - 1) / t, mt = (std::max(m.rows, m.cols) + t - 1) / t;
+    const int chain = chain_of(m, chains);
     switch (cls) {
         case kGrams: return chain == 2 ? 0 : nt * (nt + 1) / 2;
         case kSingles: return chain ? 0 : nt * (nt + 1) / 2;
@@ -910,23 +945,23 @@ uint64_t class_tiles(const MatrixSpan& m, int cls, int size)
 
 // What a launch takes, in us: a step of a tile, what a workgroup does before and behind its steps, and for a sliced tile, putting
 // a part down and taking one up.  By tile size.
-constexpr double kStepUs[2] = {0.26, 1.09}, kEndsUs[2] = {5.0, 12.0}, kPutUs[2] = {3.0, 9.0}, kTakeUs[2] = {2.0, 8.0};
+constexpr double kStepUs[kSizes] = {0.12, 0.26, 1.09}, kEndsUs[kSizes] = {3.0, 5.0, 12.0}, kPutUs[kSizes] = {2.0, 3.0, 9.0}, kTakeUs[kSizes] = {1.0, 2.0, 8.0};
 constexpr uint32_t kUnits = 256;  // compute units
 constexpr double kChainUs = 6.0, kChainStepUs = 5.0;
 
-Share share_of(const MatrixSpan* m, int count, int cls, bool large)
+Share share_of(const MatrixSpan* m, int count, bool chains, int cls, int sizes)
 {
     Share best{};
     double least = 0.0;
     uint32_t longest = 0;
     for (int i = 0; i < count; ++i)
-        if (class_tiles(m[i], cls, 0)) longest = std::max(longest, class_steps(m[i], cls));
-    for (int size = 0; size < (large ? 2 : 1); ++size)
+        if (class_tiles(m[i], chains, cls, 0)) longest = std::max(longest, class_steps(m[i], cls));
+    for (int size = 0; size < sizes; ++size)
         for (uint32_t slices = 1; slices <= kMostSlices && longest; ++slices) {
             const uint32_t len = std::max(kLeastSteps, (longest + slices - 1) / slices);
             double workgroups = 0, steps = 0, sliced = 0;
             for (int i = 0; i < count; ++i) {
-                const double tiles = (double)class_tiles(m[i], cls, size);
+                const double tiles = (double)class_tiles(m[i], chains, cls, size);
                 const uint32_t per = class_steps(m[i], cls), s = (per + len - 1) / len;
                 workgroups += tiles * s;
                 steps += tiles * per;
@@ -976,13 +1011,15 @@ Layout lay_out(const MatrixSpan* m, int count, int nsteps, int most_phase, Each&
 {
     Layout l{};
     uint64_t sum[kKinds] = {}, sums = 0;
-    bool large = false;
+    uint32_t highest = 0;
     for (int i = 0; i < count; ++i) {
-        sums += std::min<uint32_t>(m[i].rows, kMostParts);  // at most
-        large = large || std::min(m[i].rows, m[i].cols) > 256;
+        sums += norm_parts(m[i]);
+        highest = std::max(highest, std::min(m[i].rows, m[i].cols));
     }
-    const uint32_t room = large ? Large::kTile : Small::kTile;
-    for (int cls = 0; cls < kClasses; ++cls) l.share[cls] = share_of(m, count, cls, large);
+    const bool chains = highest <= kChainMost;
+    const int sizes = highest > Large::kTile ? kSizes : kSizes - 1;
+    const uint32_t room = kTileOf[sizes - 1];
+    for (int cls = 0; cls < kClasses; ++cls) l.share[cls] = share_of(m, count, chains, cls, sizes);
     size_t off = 0;
     l.items = off;  off = align256(off + (size_t)count * sizeof(Item));
     l.starts = off; off = align256(off + (size_t)count * kKinds * 4);
@@ -999,7 +1036,7 @@ Layout lay_out(const MatrixSpan* m, int count, int nsteps, int most_phase, Each&
         it.nf = np / 16;
         it.mf = mp / 16;
         it.gain = m[i].gain;
-        it.chain = (uint32_t)chain_of(m[i]);
+        it.chain = (uint32_t)chain_of(m[i], chains);
         const size_t x = (size_t)np * mp * 4;
         for (int k = 0; k < 2; ++k) {
             it.x[k] = off;  off += x;
@@ -1008,15 +1045,14 @@ Layout lay_out(const MatrixSpan* m, int count, int nsteps, int most_phase, Each&
         it.square = off;
         it.square_bytes = (size_t)np * np * 4;
         off += kSquares * it.square_bytes;
-        const size_t values = (size_t)it.n * it.m;
-        it.parts = (uint32_t)std::min<size_t>(std::min<size_t>(it.rows, kMostParts), (values + 8191) / 8192);
+        it.parts = norm_parts(m[i]);
         uint64_t units[kKinds] = {};
         units[kNorm] = it.parts;
         units[kConvert] = (uint64_t)((it.n + 63) / 64) * ((it.m + 63) / 64);
         units[kChain] = it.chain != 0;
         for (int cls = 0; cls < kClasses; ++cls) {
             const Share& s = l.share[cls];
-            if (s.workgroups) units[kProducts + cls] = class_tiles(m[i], cls, s.size) * ((class_steps(m[i], cls) + s.len - 1) / s.len);
+            if (s.workgroups) units[kProducts + cls] = class_tiles(m[i], chains, cls, s.size) * ((class_steps(m[i], cls) + s.len - 1) / s.len);
         }
         each(i, it, l.count);
         for (int k = 0; k < kKinds; ++k) l.count[k] = (uint32_t)(sum[k] += units[k]);
@@ -1027,10 +1063,10 @@ Layout lay_out(const MatrixSpan* m, int count, int nsteps, int most_phase, Each&
     for (int cls = 0; cls < kClasses; ++cls) {
         const Share& s = l.share[cls];
         bool sliced = false;
-        for (int i = 0; i < count; ++i) sliced = sliced || (class_tiles(m[i], cls, s.size) && class_steps(m[i], cls) > s.len);
+        for (int i = 0; i < count; ++i) sliced = sliced || (class_tiles(m[i], chains, cls, s.size) && class_steps(m[i], cls) > s.len);
         if (!sliced) continue;
         l.most = std::max(l.most, s.workgroups);
-        partial = std::max(partial, (size_t)s.workgroups * (s.size ? Large::kTileBytes : Small::kTileBytes));
+        partial = std::max(partial, (size_t)s.workgroups * kTileBytesOf[s.size]);
     }
     l.phase_steps = phase_steps_of(l.share, l.count[kChain] != 0, nsteps, most_phase);
     l.arrivals = align256(off);
@@ -1069,7 +1105,11 @@ hipError_t launch_product(const char* name, ProductArgs g, const Layout& places,
     const Share& share = places.share[g.cls];
     if (share.workgroups == 0) return hipSuccess;
     g.len = share.len;
-    return share.size ? launch_shared<Large, WHAT>(name, g, share.workgroups, s) : launch_shared<Small, WHAT>(name, g, share.workgroups, s);
+    switch (share.size) {
+        case 0: return launch_shared<Least, WHAT>(name, g, share.workgroups, s);
+        case 1: return launch_shared<Small, WHAT>(name, g, share.workgroups, s);
+        default: return launch_shared<Large, WHAT>(name, g, share.workgroups, s);
+    }
 }
 
 // How many times a matrix of singular values up to `bound` its planes hold: a power of two that leaves a factor of two
