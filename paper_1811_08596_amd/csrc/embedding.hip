@@ -46,11 +46,44 @@ __global__ void __launch_bounds__(256) k_embedding(EmbeddingArgs a, uint32_t lan
     }
 }
 
+// ---- rows that no token has: zeros, or the base's.  Written by workgroups beside those that sort. ----
+struct FillArgs {
+    const uint8_t* base;  // nullptr: zeros
+    uint8_t* out;
+    uint64_t chunks;      // of 16 bytes, rounded up, by row
+    uint64_t per_row;     // chunks
+    uint64_t row_values, stride;
+    int bytes;            // of an element
+};
+template <typename U>
+__device__ __forceinline__ void fill_chunk(const FillArgs& f, uint64_t i)
+{
+    constexpr uint32_t V = 16 / sizeof(U);
+    const uint64_t row = f.per_row == f.chunks ? 0 : i / f.per_row, c = (i - row * f.per_row) * V, at = row * f.stride + c;
+    U* out = reinterpret_cast<U*>(f.out) + at;
+    const U* base = f.base ? reinterpret_cast<const U*>(f.base) + at : nullptr;
+    if (c + V <= f.row_values) {
+        Run<U, V> x{};
+        if (base) x = load_run<U, V>(base);
+        store_run<U, V>(out, x);
+    } else {
+        for (uint64_t j = 0; c + j < f.row_values; ++j) out[j] = base ? base[j] : (U)0;
+    }
+}
+// chunks of the launch's share that begins at `first`, by `count` workgroups
+__device__ __forceinline__ void fill(const FillArgs& f, uint64_t first, uint64_t end, uint32_t index, uint32_t count)
+{
+    const uint64_t step = (uint64_t)count * blockDim.x;
+    uint64_t i = first + (uint64_t)index * blockDim.x + threadIdx.x;
+    if (f.bytes == 4)
+        for (; i < end; i += step) fill_chunk<uint32_t>(f, i);
+    else
+        for (; i < end; i += step) fill_chunk<uint16_t>(f, i);
+}
+
 // ---- sorting the places by token: least significant digits first, stable ----
 // A wave ranks 64 places at a time: the lanes with its own digit by one ballot per bit, the earlier groups' by a count.
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
-constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
-constexpr uint32_t kSortBlock = 4096;  // places a workgroup has
 
 __device__ __forceinline__ uint64_t same_digit(uint32_t digit, bool present)
 {
@@ -62,6 +95,40 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t digit, bool present)
     }
     return m;
 }
+// the place of a group's items among those of their digit that the wave has had before; counts them
+template <typename U>
+__device__ __forceinline__ uint32_t rank_in_wave(U* wave_count, uint32_t digit, bool present, uint32_t lane)
+{
+    const uint64_t same = same_digit(digit, present), lower = same & ((1ull << lane) - 1ull);
+    uint32_t old = 0;
+    if (present) old = wave_count[digit];
+    // every lane has read before the first of each digit writes: a wave's LDS accesses are done in order, and the fences keep
+    // the compiler to it
+    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (present && lower == 0) wave_count[digit] = (U)(old + (uint32_t)__popcll(same));
+    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    return old + (uint32_t)__popcll(lower);
+}
+// exclusive sums of one value a thread of the first kDigits threads; `scan`: kDigits / 64 words
+__device__ __forceinline__ uint32_t digits_before(uint32_t v, uint32_t* scan)
+{
+    const uint32_t tid = threadIdx.x, lane = tid & 63u;
+    uint32_t sum = v;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t u = __shfl_up(sum, d);
+        if (lane >= (uint32_t)d) sum += u;
+    }
+    if (tid < kDigits && lane == 63) scan[tid >> 6] = sum;
+    __syncthreads();
+    uint32_t before = 0;
+    for (uint32_t w = 0; w < kDigits / 64; ++w)
+        if (w < tid >> 6) before += scan[w];
+    __syncthreads();
+    return before + sum - v;
+}
 
 struct SortArgs {
     const void* tokens;
@@ -71,22 +138,107 @@ struct SortArgs {
     uint2* b;
     uint32_t* counts;    // [passes][blocks][kDigits]
     int passes;
+    FillArgs fill;
 };
+
+// up to kSortOne places: one workgroup, all passes in LDS; the others fill
+constexpr uint32_t kOneThreads = 1024, kOneWaves = kOneThreads / 64, kOneGroups = 8, kSortOne = kOneThreads * kOneGroups;
+__global__ void __launch_bounds__(kOneThreads) k_sort_one(SortArgs s)
+{
+    __shared__ uint32_t keys[kSortOne];  // 64 KB with the rest: two workgroups to a compute unit
+    __shared__ uint16_t places[kSortOne];
+    __shared__ uint16_t wave_count[kOneWaves][kDigits];
+    __shared__ uint32_t scan[kDigits / 64];
+    if (blockIdx.x) {
+        fill(s.fill, 0, s.fill.chunks, blockIdx.x - 1, gridDim.x - 1);
+        return;
+    }
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
+    const uint32_t groups = (s.count + kOneThreads - 1) / kOneThreads;  // of 64 places that a wave has
+    uint2 item[kOneGroups];
+#pragma unroll
+    for (uint32_t g = 0; g < kOneGroups; ++g) {
+        if (g >= groups) break;
+        const uint32_t i = (wave * groups + g) * 64 + lane;
+        item[g] = make_uint2(i < s.count ? token_row(s.tokens, s.token_bits, i, s.rows) : 0xFFFFFFFFu, i);
+    }
+    for (int pass = 0; pass < s.passes; ++pass) {
+        const int shift = pass * kDigitBits;
+        for (uint32_t i = tid; i < kOneWaves * kDigits / 2; i += kOneThreads) reinterpret_cast<uint32_t*>(&wave_count[0][0])[i] = 0;
+        __syncthreads();
+        uint32_t rank[kOneGroups];
+#pragma unroll
+        for (uint32_t g = 0; g < kOneGroups; ++g) {
+            if (g >= groups) break;
+            const bool present = (wave * groups + g) * 64 + lane < s.count;
+            rank[g] = rank_in_wave(wave_count[wave], (item[g].x >> shift) & (kDigits - 1u), present, lane);
+        }
+        __syncthreads();
+        uint32_t total = 0;
+        if (tid < kDigits)
+#pragma unroll
+            for (uint32_t w = 0; w < kOneWaves; ++w) total += wave_count[w][tid];
+        uint32_t sum = digits_before(total, scan);
+        if (tid < kDigits)
+#pragma unroll
+            for (uint32_t w = 0; w < kOneWaves; ++w) {
+                const uint32_t c = wave_count[w][tid];
+                wave_count[w][tid] = (uint16_t)sum;
+                sum += c;
+            }
+        __syncthreads();
+#pragma unroll
+        for (uint32_t g = 0; g < kOneGroups; ++g)
+            if (g < groups && (wave * groups + g) * 64 + lane < s.count) {
+                const uint32_t at = wave_count[wave][(item[g].x >> shift) & (kDigits - 1u)] + rank[g];
+                keys[at] = item[g].x;
+                places[at] = (uint16_t)item[g].y;
+            }
+        __syncthreads();
+#pragma unroll
+        for (uint32_t g = 0; g < kOneGroups; ++g) {
+            if (g >= groups) break;
+            const uint32_t i = (wave * groups + g) * 64 + lane;
+            if (i < s.count) item[g] = make_uint2(keys[i], places[i]);
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (uint32_t g = 0; g < kOneGroups; ++g) {
+        if (g >= groups) break;
+        const uint32_t i = (wave * groups + g) * 64 + lane;
+        if (i < s.count) s.a[i] = item[g];
+    }
+}
+
+// more places: workgroups of kSortBlock places, a launch a pass behind one that counts; other workgroups fill a share in each
+constexpr int kSortThreads = kDigits, kSortWaves = kSortThreads / 64;
+constexpr uint32_t kSortBlock = 2048, kGroups = kSortBlock / kSortThreads;
+
+__device__ __forceinline__ bool fill_share(const SortArgs& s, int launch)
+{
+    if (blockIdx.x < s.blocks) return false;
+    const uint64_t launches = (uint64_t)s.passes + 1, first = s.fill.chunks * launch / launches, end = s.fill.chunks * (launch + 1) / launches;
+    fill(s.fill, first, end, blockIdx.x - s.blocks, gridDim.x - s.blocks);
+    return true;
+}
 
 // counts of the first digit, block by block; clears the later passes' counts
 __global__ void __launch_bounds__(kSortThreads) k_sort_count(SortArgs s)
 {
     __shared__ uint32_t hist[kDigits];
-    for (uint32_t i = threadIdx.x; i < kDigits; i += kSortThreads) hist[i] = 0;
+    if (fill_share(s, 0)) return;
+    const uint32_t tid = threadIdx.x, at = blockIdx.x * kSortBlock;
+    hist[tid] = 0;
     __syncthreads();
-    const uint32_t at = blockIdx.x * kSortBlock;
-    for (uint32_t i = threadIdx.x; i < kSortBlock; i += kSortThreads)
-        if (at + i < s.count) atomicAdd(&hist[token_row(s.tokens, s.token_bits, at + i, s.rows) & (kDigits - 1u)], 1u);
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < kDigits; i += kSortThreads) {
-        s.counts[(size_t)blockIdx.x * kDigits + i] = hist[i];
-        for (int p = 1; p < s.passes; ++p) s.counts[((size_t)p * s.blocks + blockIdx.x) * kDigits + i] = 0;
+#pragma unroll
+    for (uint32_t g = 0; g < kGroups; ++g) {
+        const uint32_t i = at + g * kSortThreads + tid;
+        if (i < s.count) atomicAdd(&hist[token_row(s.tokens, s.token_bits, i, s.rows) & (kDigits - 1u)], 1u);
     }
+    __syncthreads();
+    s.counts[(size_t)blockIdx.x * kDigits + tid] = hist[tid];
+    for (int p = 1; p < s.passes; ++p) s.counts[((size_t)p * s.blocks + blockIdx.x) * kDigits + tid] = 0;
 }
 
 // one pass: every workgroup finds where its digits begin from all blocks' counts, and counts the next pass's digits by the
@@ -94,69 +246,58 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_count(SortArgs s)
 __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortArgs s, int pass)
 {
     __shared__ uint32_t wave_count[kSortWaves][kDigits];
-    __shared__ uint32_t base[kDigits];
-    __shared__ uint32_t scan[kDigits];
+    __shared__ uint32_t scan[kDigits / 64];
+    if (fill_share(s, pass + 1)) return;
     const uint32_t tid = threadIdx.x, wave = tid >> 6, lane = tid & 63u;
     const uint2* from = pass & 1 ? s.b : s.a;
     uint2* to = pass & 1 ? s.a : s.b;
-    const uint32_t* counts = s.counts + (size_t)pass * s.blocks * kDigits;
+    const uint32_t* counts = s.counts + (size_t)pass * s.blocks * kDigits + tid;
     uint32_t* next = pass + 1 < s.passes ? s.counts + (size_t)(pass + 1) * s.blocks * kDigits : nullptr;
-    for (uint32_t i = tid; i < kSortWaves * kDigits; i += kSortThreads) (&wave_count[0][0])[i] = 0;
-    uint32_t before = 0, total = 0;
-    if (tid < kDigits)
-        for (uint32_t b = 0; b < s.blocks; ++b) {
-            const uint32_t c = counts[(size_t)b * kDigits + tid];
-            if (b < blockIdx.x) before += c;
-            total += c;
-        }
-    if (tid < kDigits) scan[tid] = total;
-    __syncthreads();
-    for (uint32_t d = 1; d < kDigits; d <<= 1) {  // inclusive sums
-        const uint32_t v = tid < kDigits && tid >= d ? scan[tid - d] : 0;
-        __syncthreads();
-        if (tid < kDigits) scan[tid] += v;
-        __syncthreads();
-    }
-    if (tid < kDigits) base[tid] = scan[tid] - total + before;
     // a wave's share: consecutive groups of 64 places
-    constexpr uint32_t kGroups = kSortBlock / kSortThreads;
     uint2 item[kGroups];
+#pragma unroll
+    for (uint32_t g = 0; g < kGroups; ++g) {
+        const uint32_t i = blockIdx.x * kSortBlock + (wave * kGroups + g) * 64 + lane;
+        item[g] = make_uint2(0xFFFFFFFFu, i);
+        if (i < s.count) item[g] = pass ? from[i] : make_uint2(token_row(s.tokens, s.token_bits, i, s.rows), i);
+    }
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) wave_count[w][tid] = 0;
+    uint32_t before = 0, total = 0, b = 0;
+    for (; b + 16 <= s.blocks; b += 16) {
+        uint32_t c[16];
+#pragma unroll
+        for (int u = 0; u < 16; ++u) c[u] = counts[(size_t)(b + u) * kDigits];
+#pragma unroll
+        for (int u = 0; u < 16; ++u) {
+            if (b + u < blockIdx.x) before += c[u];
+            total += c[u];
+        }
+    }
+    for (; b < s.blocks; ++b) {
+        const uint32_t c = counts[(size_t)b * kDigits];
+        if (b < blockIdx.x) before += c;
+        total += c;
+    }
+    uint32_t sum = digits_before(total, scan) + before;  // a barrier within: wave_count is clear
     uint32_t rank[kGroups];
     const int shift = pass * kDigitBits;
 #pragma unroll
     for (uint32_t g = 0; g < kGroups; ++g) {
-        const uint32_t i = blockIdx.x * kSortBlock + wave * (kGroups * 64) + g * 64 + lane;
-        const bool present = i < s.count;
-        item[g] = make_uint2(0xFFFFFFFFu, i);
-        if (present) item[g] = pass ? from[i] : make_uint2(token_row(s.tokens, s.token_bits, i, s.rows), i);
-        const uint32_t digit = (item[g].x >> shift) & (kDigits - 1u);
-        const uint64_t same = same_digit(digit, present);
-        uint32_t old = 0;
-        if (present) {
-            old = wave_count[wave][digit];
-            rank[g] = old + (uint32_t)__popcll(same & ((1ull << lane) - 1ull));
-        }
-        // every lane has read before the first of each digit writes: a wave's LDS accesses are done in order, and the fences
-        // keep the compiler to it
-        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        if (present && (same & ((1ull << lane) - 1ull)) == 0) wave_count[wave][digit] = old + (uint32_t)__popcll(same);
-        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+        const bool present = blockIdx.x * kSortBlock + (wave * kGroups + g) * 64 + lane < s.count;
+        rank[g] = rank_in_wave(wave_count[wave], (item[g].x >> shift) & (kDigits - 1u), present, lane);
     }
     __syncthreads();
-    if (tid < kDigits) {
-        uint32_t sum = base[tid];
-        for (int w = 0; w < kSortWaves; ++w) {
-            const uint32_t c = wave_count[w][tid];
-            wave_count[w][tid] = sum;
-            sum += c;
-        }
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+        const uint32_t c = wave_count[w][tid];
+        wave_count[w][tid] = sum;
+        sum += c;
     }
     __syncthreads();
 #pragma unroll
     for (uint32_t g = 0; g < kGroups; ++g) {
-        const uint32_t i = blockIdx.x * kSortBlock + wave * (kGroups * 64) + g * 64 + lane;
+        const uint32_t i = blockIdx.x * kSortBlock + (wave * kGroups + g) * 64 + lane;
         if (i >= s.count) continue;
         const uint32_t at = wave_count[wave][(item[g].x >> shift) & (kDigits - 1u)] + rank[g];
         to[at] = item[g];
@@ -164,22 +305,8 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortArgs s, int p
     }
 }
 
-// ---- rows that no token has: zeros, or the base's ----
-template <typename T, int V>
-__global__ void __launch_bounds__(256) k_fill_rows(const T* base, T* out, size_t rows, uint32_t width, size_t stride, uint32_t lanes)
-{
-    const uint32_t li = threadIdx.x & (lanes - 1u), per = 256u / lanes;
-    for (size_t r = (size_t)blockIdx.x * per + threadIdx.x / lanes; r < rows; r += (size_t)gridDim.x * per)
-        for (uint32_t c = li * V; c < width; c += lanes * V) {
-            if (c + V <= width) {
-                Run<T, V> x{};
-                if (base) x = load_run<T, V>(base + r * stride + c);
-                store_run<T, V>(out + r * stride + c, x);
-            } else {
-                for (uint32_t j = c; j < width; ++j) out[r * stride + j] = base ? base[r * stride + j] : from_float<T>(0.f);
-            }
-        }
-}
+// nothing to sort
+__global__ void __launch_bounds__(kOneThreads) k_fill(FillArgs f) { fill(f, 0, f.chunks, blockIdx.x, gridDim.x); }
 
 // ---- sums over the sorted places ----
 struct SumArgs {
@@ -194,15 +321,15 @@ struct SumArgs {
     float* partial;  // [stretches][2][width]: what a run that began before the stretch has in it; what a run has that goes on behind it
 };
 
-template <typename TI, typename TO, int V>
-__device__ __forceinline__ void write_row(const SumArgs& a, uint32_t row, uint32_t c, uint32_t n, const float* acc)
+// there: the row's present values, where they are added and all V columns are
+template <typename TO, int V>
+__device__ __forceinline__ void write_row(const SumArgs& a, uint32_t row, uint32_t c, uint32_t n, const float* acc, const Run<TO, V>& there)
 {
     TO* dst = static_cast<TO*>(a.out) + (size_t)row * a.out_stride + c;
     if (n == V) {
-        Run<TO, V> y{};
-        if (a.add) y = load_run<TO, V>(dst);
+        Run<TO, V> y;
 #pragma unroll
-        for (int i = 0; i < V; ++i) y.v[i] = from_float<TO>(a.add ? to_float(y.v[i]) + acc[i] * a.scale : acc[i] * a.scale);
+        for (int i = 0; i < V; ++i) y.v[i] = from_float<TO>(a.add ? to_float(there.v[i]) + acc[i] * a.scale : acc[i] * a.scale);
         store_run<TO, V>(dst, y);
     } else {
 #pragma unroll
@@ -214,11 +341,20 @@ template <int V>
 __device__ __forceinline__ void write_partial(const SumArgs& a, uint32_t stretch, uint32_t which, uint32_t c, uint32_t n, const float* acc)
 {
     float* dst = a.partial + ((size_t)stretch * 2 + which) * a.width + c;
+    if (n == V) {
+        Run<float, V> r;
 #pragma unroll
-    for (uint32_t i = 0; i < V; ++i)
-        if (i < n) dst[i] = acc[i];
+        for (int i = 0; i < V; ++i) r.v[i] = acc[i];
+        store_run<float, V>(dst, r);
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < V; ++i)
+            if (i < n) dst[i] = acc[i];
+    }
 }
 
+// A wave has a stretch of the sorted places and 64 V columns; kAhead rows are on their way together.
+constexpr uint32_t kAhead = 8;
 template <typename TI, typename TO, int V>
 __global__ void __launch_bounds__(256) k_sum_stretches(SumArgs a, uint32_t slabs)
 {
@@ -232,70 +368,234 @@ __global__ void __launch_bounds__(256) k_sum_stretches(SumArgs a, uint32_t slabs
     float acc[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) acc[i] = 0.f;
-    uint32_t run = a.sorted[first].x;                     // uniform: the run being summed
-    bool head = first > 0 && a.sorted[first - 1].x == run;  // it began before this stretch
-    for (uint32_t p = first; p < end; ++p) {
-        const uint2 it = a.sorted[p];
-        if (it.x != run) {
-            if (run < a.rows) {
-                if (head) write_partial<V>(a, stretch, 0, c, n, acc);
-                else write_row<TI, TO, V>(a, run, c, n, acc);
+    bool head = false;  // the run began before this stretch
+    for (uint32_t at = first; at < end; at += 64u) {
+        const uint32_t here = min(64u, end - at);
+        const uint2 own = a.sorted[at + min(lane, here - 1)];
+        const uint32_t behind = at + here < a.count ? a.sorted[at + here].x : a.rows;
+        if (at == first) head = first > 0 && a.sorted[first - 1].x == (uint32_t)__builtin_amdgcn_readfirstlane((int)own.x);
+        for (uint32_t p = 0; p < here; p += kAhead) {
+            Run<TI, V> x[kAhead];
+            Run<TO, V> y[kAhead];
+            uint32_t row[kAhead + 1];
+#pragma unroll
+            for (uint32_t u = 0; u <= kAhead; ++u)
+                row[u] = p + u < here ? (uint32_t)__builtin_amdgcn_readlane((int)own.x, (int)(p + u)) : behind;
+#pragma unroll
+            for (uint32_t u = 0; u < kAhead; ++u) {
+                const uint32_t place = (uint32_t)__builtin_amdgcn_readlane((int)own.y, (int)min(p + u, here - 1));
+                const TI* r = src + (size_t)place * a.source_stride;
+                if (n == V) {
+                    x[u] = load_run<TI, V>(r);
+                    // what is in the table's row already, where a run ends
+                    if (a.add && p + u < here && row[u] != row[u + 1] && row[u] < a.rows)
+                        y[u] = load_run<TO, V>(static_cast<const TO*>(a.out) + (size_t)row[u] * a.out_stride + c);
+                } else {
+#pragma unroll
+                    for (uint32_t i = 0; i < V; ++i) x[u].v[i] = i < n ? r[i] : TI{};
+                }
             }
 #pragma unroll
-            for (int i = 0; i < V; ++i) acc[i] = 0.f;
-            run = it.x;
-            head = false;
-        }
-        if (run >= a.rows) return;                        // tokens outside the table are sorted last
-        if (n == V) {
-            const Run<TI, V> x = load_run<TI, V>(src + (size_t)it.y * a.source_stride);
+            for (uint32_t u = 0; u < kAhead; ++u) {
+                if (p + u >= here) break;
+                if (row[u] >= a.rows) return;  // tokens outside the table are sorted last
 #pragma unroll
-            for (int i = 0; i < V; ++i) acc[i] += to_float(x.v[i]);
-        } else {
+                for (int i = 0; i < V; ++i) acc[i] += to_float(x[u].v[i]);
+                const bool last = at + p + u + 1 == end;
+                if (row[u] == row[u + 1] && !last) continue;
+                if (head) write_partial<V>(a, stretch, 0, c, n, acc);
+                else if (row[u] == row[u + 1]) write_partial<V>(a, stretch, 1, c, n, acc);
+                else write_row<TO, V>(a, row[u], c, n, acc, y[u]);
 #pragma unroll
-            for (uint32_t i = 0; i < V; ++i)
-                if (i < n) acc[i] += to_float(src[(size_t)it.y * a.source_stride + i]);
+                for (int i = 0; i < V; ++i) acc[i] = 0.f;
+                head = false;
+            }
         }
     }
-    if (run >= a.rows) return;
-    const bool tail = end < a.count && a.sorted[end].x == run;  // it goes on behind this stretch
-    if (head) write_partial<V>(a, stretch, 0, c, n, acc);
-    else if (tail) write_partial<V>(a, stretch, 1, c, n, acc);
-    else write_row<TI, TO, V>(a, run, c, n, acc);
 }
 
-// runs that cross stretches: a workgroup per stretch in which one begins and goes on, and per slab of 64 V columns
+// runs that cross stretches: a workgroup per stretch in which one begins and goes on, and per slab of 64 V columns; its
+// waves have every fourth part, in order
 template <typename TI, typename TO, int V>
-__global__ void __launch_bounds__(1024) k_join_runs(SumArgs a)
+__global__ void __launch_bounds__(256) k_join_runs(SumArgs a)
 {
-    __shared__ float part[16][64 * V];
-    const uint32_t stretch = blockIdx.x, lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    __shared__ float part[3][64 * V];
+    const uint32_t stretch = blockIdx.x, lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t first = stretch * a.stretch, end = first + a.stretch;
     if (end >= a.count) return;
-    const uint32_t run = a.sorted[end].x;
-    if (run >= a.rows || a.sorted[end - 1].x != run) return;
-    if (first > 0 && a.sorted[first].x == run && a.sorted[first - 1].x == run) return;  // it began earlier
-    uint32_t last = stretch + 1;  // the last stretch that the run reaches
-    while (last + 1 < a.stretches && a.sorted[(last + 1) * a.stretch].x == run) ++last;
+    const uint32_t run = a.sorted[end].x, inside = a.sorted[end - 1].x, begin = a.sorted[first].x, earlier = first ? a.sorted[first - 1].x : run + 1;
+    if (run >= a.rows || inside != run || (begin == run && earlier == run)) return;  // none, or it began earlier
+    // the last stretch that the run reaches: 64 of the stretches' first places at a time
+    uint32_t last = stretch + 1;
+    for (uint32_t s = stretch + 1;; s += 64u) {
+        const uint32_t t = s + lane;
+        const uint64_t in = __ballot(t < a.stretches && a.sorted[(size_t)t * a.stretch].x == run);
+        const uint32_t k = in == ~0ull ? 64u : (uint32_t)__builtin_ctzll(~in);
+        if (k) last = s + k - 1;
+        if (k < 64) break;
+    }
     const uint32_t c = (blockIdx.y * 64u + lane) * V;
     const uint32_t n = c >= a.width ? 0u : min((uint32_t)V, a.width - c);
     float acc[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) acc[i] = 0.f;
-    for (uint32_t s = stretch + wave; s <= last; s += 16u) {
-        const float* p = a.partial + ((size_t)s * 2 + (s == stretch ? 1u : 0u)) * a.width + c;
+    for (uint32_t s = stretch + wave; s <= last; s += 4u * 4u) {
+        Run<float, V> x[4];
 #pragma unroll
-        for (uint32_t i = 0; i < V; ++i)
-            if (i < n) acc[i] += p[i];
+        for (uint32_t u = 0; u < 4; ++u) {
+            const uint32_t t = min(s + 4u * u, last);
+            const float* p = a.partial + ((size_t)t * 2 + (t == stretch ? 1u : 0u)) * a.width + c;
+            if (n == V) {
+                x[u] = load_run<float, V>(p);
+            } else {
+#pragma unroll
+                for (uint32_t i = 0; i < V; ++i) x[u].v[i] = i < n ? p[i] : 0.f;
+            }
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u)
+            if (s + 4u * u <= last)
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[i] += x[u].v[i];
     }
+    if (wave)
 #pragma unroll
-    for (int i = 0; i < V; ++i) part[wave][lane * V + i] = acc[i];
+        for (int i = 0; i < V; ++i) part[wave - 1][lane * V + i] = acc[i];
     __syncthreads();
     if (wave) return;
-    for (int w = 1; w < 16; ++w)
+    for (int w = 0; w < 3; ++w)
 #pragma unroll
         for (int i = 0; i < V; ++i) acc[i] += part[w][lane * V + i];
-    write_row<TI, TO, V>(a, run, c, n, acc);
+    Run<TO, V> there{};
+    if (a.add && n == V) there = load_run<TO, V>(static_cast<const TO*>(a.out) + (size_t)run * a.out_stride + c);
+    write_row<TO, V>(a, run, c, n, acc, there);
+}
+
+// ---- up to kFew places: no sorting, one launch ----
+// A workgroup per place and slab of 64 V columns compares its token with all others; if it is the first with that token, it sums
+// the rows of all of them, its waves eight rows at a time in turn.  Other workgroups fill the rows that no token has.
+constexpr uint32_t kFew = 1024, kFewRows = 16384;  // places; rows that one workgroup fills at most
+struct FewArgs {
+    EmbeddingArgs e;  // source: the rows' gradients, out: the table's
+    uint32_t slabs, fillers, per_filler, lanes;
+};
+template <typename TI, typename TO, int V>
+__global__ void __launch_bounds__(256) k_gradient_few(FewArgs f)
+{
+    const EmbeddingArgs& a = f.e;
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6), count = (uint32_t)a.ntokens;
+    const TO* base = static_cast<const TO*>(a.base);
+    TO* out = static_cast<TO*>(a.out);
+    if (blockIdx.x >= count * f.slabs) {
+        __shared__ uint32_t has[kFewRows / 32];
+        const uint64_t first = (uint64_t)(blockIdx.x - count * f.slabs) * f.per_filler, end = min((uint64_t)a.rows, first + f.per_filler);
+        for (uint32_t i = tid; i < (f.per_filler + 31u) / 32u; i += 256) has[i] = 0;
+        __syncthreads();
+        for (uint32_t t = tid; t < count; t += 256) {
+            const uint32_t row = token_row(a.tokens, a.token_bits, t, (uint32_t)a.rows);
+            if (row >= first && row < end) atomicOr(&has[(row - first) / 32u], 1u << ((row - first) & 31u));
+        }
+        __syncthreads();
+        constexpr uint32_t W = 16 / sizeof(TO);
+        const uint32_t li = tid & (f.lanes - 1u), per = 256u / f.lanes;
+        for (uint64_t row = first + tid / f.lanes; row < end; row += per) {
+            if (has[(row - first) / 32u] >> ((row - first) & 31u) & 1u) continue;
+            for (uint32_t c = li * W; c < a.width; c += f.lanes * W) {
+                const uint64_t at = row * a.out_stride + c;
+                if (c + W <= a.width) {
+                    Run<TO, W> x{};
+                    if (base) x = load_run<TO, W>(base + at);
+                    store_run<TO, W>(out + at, x);
+                } else {
+                    for (uint32_t j = 0; c + j < a.width; ++j) out[at + j] = base ? base[at + j] : TO{};
+                }
+            }
+        }
+        return;
+    }
+    __shared__ uint64_t same[kFew / 64];
+    __shared__ uint16_t places[kFew];
+    __shared__ float part[3][64 * V];
+    const uint32_t place = blockIdx.x / f.slabs, slab = blockIdx.x - place * f.slabs;
+    const uint32_t row = token_row(a.tokens, a.token_bits, place, (uint32_t)a.rows);
+    if (row >= a.rows) return;
+    const uint32_t c = (slab * 64u + lane) * V, n = c >= a.width ? 0u : min((uint32_t)V, a.width - c);
+    const uint64_t at = (uint64_t)row * a.out_stride + c;
+    Run<TO, V> there{};
+    if (base && wave == 0) {
+        if (n == V) there = load_run<TO, V>(base + at);
+        else
+#pragma unroll
+            for (uint32_t i = 0; i < V; ++i)
+                if (i < n) there.v[i] = base[at + i];
+    }
+    uint32_t mine = 0;  // which of this lane's places have the token
+#pragma unroll
+    for (uint32_t k = 0; k < kFew / 256; ++k) {
+        const uint32_t t = k * 256 + tid;
+        const bool is = t < count && token_row(a.tokens, a.token_bits, t, (uint32_t)a.rows) == row;
+        const uint64_t m = __ballot(is);
+        if (lane == 0) same[k * 4 + wave] = m;
+        mine |= (is ? 1u : 0u) << k;
+    }
+    __syncthreads();
+    uint32_t total = 0, before = 0;  // places of the token; those before this one
+#pragma unroll
+    for (uint32_t i = 0; i < kFew / 64; ++i) {
+        const uint64_t m = same[i];
+        before += i * 64 + 64 <= place ? (uint32_t)__popcll(m) : i * 64 <= place ? (uint32_t)__popcll(m & ((1ull << (place & 63u)) - 1ull)) : 0u;
+        total += (uint32_t)__popcll(m);
+    }
+    if (before) return;  // another workgroup's
+#pragma unroll
+    for (uint32_t k = 0; k < kFew / 256; ++k)
+        if (mine >> k & 1u) {
+            uint32_t r = (uint32_t)__popcll(same[k * 4 + wave] & ((1ull << lane) - 1ull));
+            for (uint32_t i = 0; i < k * 4 + wave; ++i) r += (uint32_t)__popcll(same[i]);
+            places[r] = (uint16_t)(k * 256 + tid);
+        }
+    __syncthreads();
+    float acc[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[i] = 0.f;
+    const TI* src = static_cast<const TI*>(a.source) + c;
+    for (uint32_t p = wave * kAhead; p < total; p += 4 * kAhead) {
+        Run<TI, V> x[kAhead];
+#pragma unroll
+        for (uint32_t u = 0; u < kAhead; ++u) {
+            const TI* r = src + (size_t)__builtin_amdgcn_readfirstlane(places[min(p + u, total - 1)]) * a.source_stride;
+            if (n == V) {
+                x[u] = load_run<TI, V>(r);
+            } else {
+#pragma unroll
+                for (uint32_t i = 0; i < V; ++i) x[u].v[i] = i < n ? r[i] : TI{};
+            }
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < kAhead; ++u)
+            if (p + u < total)
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[i] += to_float(x[u].v[i]);
+    }
+    if (total > kAhead) {
+        if (wave)
+#pragma unroll
+            for (int i = 0; i < V; ++i) part[wave - 1][lane * V + i] = acc[i];
+        __syncthreads();
+        if (wave == 0)
+            for (int w = 0; w < 3; ++w)
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[i] += part[w][lane * V + i];
+    }
+    if (wave) return;
+    Run<TO, V> y;
+#pragma unroll
+    for (int i = 0; i < V; ++i) y.v[i] = from_float<TO>(base ? to_float(there.v[i]) + acc[i] * a.scale : acc[i] * a.scale);
+    if (n == V) store_run<TO, V>(out + at, y);
+    else
+#pragma unroll
+        for (uint32_t i = 0; i < V; ++i)
+            if (i < n) out[at + i] = y.v[i];
 }
 
 int sort_passes(size_t rows)
@@ -313,6 +613,8 @@ uint32_t lanes_for(uint32_t width, uint32_t v)
 // values a lane has of a row of type bytes: 16 bytes
 constexpr int values_of(size_t bytes) { return bytes == 4 ? 4 : 8; }
 
+constexpr uint32_t kFillThreads = 256 * 2048;  // that fill at once: what the card holds
+
 struct GradientPlan {
     uint32_t blocks, stretch, stretches;
     int passes;
@@ -324,8 +626,8 @@ GradientPlan gradient_plan(size_t rows, uint32_t width, size_t count)
     p.passes = sort_passes(rows);
     p.blocks = (uint32_t)((count + kSortBlock - 1) / kSortBlock);
     const size_t slabs = (width + 511u) / 512u;
-    p.stretch = 8;
-    while (count * slabs / p.stretch > 8192) p.stretch *= 2;
+    p.stretch = 16;
+    while (count * slabs / p.stretch > 4096) p.stretch *= 2;
     p.stretches = (uint32_t)((count + p.stretch - 1) / p.stretch);
     size_t off = 0;
     p.a = off;       off = align256(off + count * 8);
@@ -361,30 +663,54 @@ size_t embedding_gradient_workspace(size_t rows, uint32_t width, size_t ntokens)
 
 hipError_t launch_embedding_gradient(const EmbeddingArgs& a, uint8_t* ws, hipStream_t s)
 {
-    hipError_t e = hipSuccess;
+    FillArgs f{};
     if (a.base != a.out) {
-        e = with_type(a.out_type, [&](auto to) {
-            using TO = decltype(to);
-            constexpr int V = values_of(sizeof(TO));
-            const uint32_t lanes = lanes_for(a.width, V), per = 256u / lanes;
-            const dim3 grid((uint32_t)std::min<size_t>((a.rows + per - 1) / per, 4096));
-            FFTSP_LAUNCH("embedding_fill", (k_fill_rows<TO, V>), grid, dim3(256), 0, s, static_cast<const TO*>(a.base),
-                         static_cast<TO*>(a.out), a.rows, a.width, a.out_stride, lanes);
-            return hipGetLastError();
-        });
-        if (e != hipSuccess) return e;
+        const bool flat = a.out_stride == a.width;
+        f.bytes = type_bytes(a.out_type);
+        f.base = static_cast<const uint8_t*>(a.base);
+        f.out = static_cast<uint8_t*>(a.out);
+        f.row_values = flat ? (uint64_t)a.rows * a.width : a.width;
+        f.stride = a.out_stride;
+        f.per_row = (f.row_values * f.bytes + 15) / 16;
+        f.chunks = f.per_row * (flat ? 1 : a.rows);
     }
-    if (a.ntokens == 0) return hipSuccess;
+    auto fillers = [&](uint64_t chunks, uint32_t threads) { return (uint32_t)std::min<uint64_t>((chunks + threads - 1) / threads, kFillThreads / threads); };
+    if (a.ntokens == 0) {
+        if (f.chunks) FFTSP_LAUNCH("embedding_fill", k_fill, dim3(fillers(f.chunks, kOneThreads)), dim3(kOneThreads), 0, s, f);
+        return hipGetLastError();
+    }
+    if (a.ntokens <= kFew) {
+        return with_type(a.source_type, [&](auto ti) {
+            return with_type(a.out_type, [&](auto to) {
+                using TI = decltype(ti);
+                using TO = decltype(to);
+                constexpr int V = values_of(sizeof(TI));
+                FewArgs w{a, (a.width + 64u * V - 1u) / (64u * V), 0, 0, lanes_for(a.width, 16 / sizeof(TO))};
+                if (a.base != a.out) {
+                    // as many workgroups as fill the card, or more where their bitmaps would not hold the rows
+                    w.per_filler = (uint32_t)std::min<uint64_t>(kFewRows, (a.rows + 2047) / 2048);
+                    w.fillers = (uint32_t)((a.rows + w.per_filler - 1) / w.per_filler);
+                }
+                FFTSP_LAUNCH("embedding_few", (k_gradient_few<TI, TO, V>), dim3((uint32_t)a.ntokens * w.slabs + w.fillers), dim3(256), 0, s, w);
+                return hipGetLastError();
+            });
+        });
+    }
     const GradientPlan p = gradient_plan(a.rows, a.width, a.ntokens);
     SortArgs so{a.tokens, a.token_bits, (uint32_t)a.rows, (uint32_t)a.ntokens, p.blocks, reinterpret_cast<uint2*>(ws + p.a),
-                reinterpret_cast<uint2*>(ws + p.b), reinterpret_cast<uint32_t*>(ws + p.counts), p.passes};
-    FFTSP_LAUNCH("embedding_sort_count", k_sort_count, dim3(p.blocks), dim3(kSortThreads), 0, s, so);
-    for (int i = 0; i < p.passes; ++i)
-        FFTSP_LAUNCH("embedding_sort", k_sort_scatter, dim3(p.blocks), dim3(kSortThreads), 0, s, so, i);
-    e = hipGetLastError();
+                reinterpret_cast<uint2*>(ws + p.b), reinterpret_cast<uint32_t*>(ws + p.counts), p.passes, f};
+    const bool one = so.count <= kSortOne;
+    if (one) {
+        FFTSP_LAUNCH("embedding_sort_one", k_sort_one, dim3(1 + fillers(f.chunks, kOneThreads)), dim3(kOneThreads), 0, s, so);
+    } else {
+        const dim3 grid(p.blocks + fillers(f.chunks / (p.passes + 1) + 1, kSortThreads) * (f.chunks ? 1 : 0));
+        FFTSP_LAUNCH("embedding_sort_count", k_sort_count, grid, dim3(kSortThreads), 0, s, so);
+        for (int i = 0; i < p.passes; ++i) FFTSP_LAUNCH("embedding_sort", k_sort_scatter, grid, dim3(kSortThreads), 0, s, so, i);
+    }
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     SumArgs m{};
-    m.sorted = p.passes & 1 ? so.b : so.a;
+    m.sorted = !one && p.passes & 1 ? so.b : so.a;
     m.count = so.count;
     m.stretch = p.stretch;
     m.stretches = p.stretches;
@@ -405,8 +731,7 @@ hipError_t launch_embedding_gradient(const EmbeddingArgs& a, uint8_t* ws, hipStr
             const uint32_t slabs = (a.width + 64u * V - 1u) / (64u * V);
             const uint64_t waves = (uint64_t)p.stretches * slabs;
             FFTSP_LAUNCH("embedding_sum", (k_sum_stretches<TI, TO, V>), dim3((uint32_t)((waves + 3) / 4)), dim3(256), 0, s, m, slabs);
-            if (p.stretches > 1)
-                FFTSP_LAUNCH("embedding_join", (k_join_runs<TI, TO, V>), dim3(p.stretches, slabs), dim3(1024), 0, s, m);
+            if (p.stretches > 1) FFTSP_LAUNCH("embedding_join", (k_join_runs<TI, TO, V>), dim3(p.stretches, slabs), dim3(256), 0, s, m);
             return hipGetLastError();
         });
     });

@@ -358,34 +358,45 @@ def decompress_segments(packed, packed_nbytes: int, grad_out, seg_offsets, theta
 F32, BF16, F16 = range(3)
 
 
-def _type(t) -> int:
+_TYPES: dict = {}   # torch's types as fftsp_type, filled at the first call (torch is not loaded at import)
+_INDEX: dict = {}
+
+
+def _learn_types():
     import torch
-    code = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}.get(t.dtype)
+    _TYPES.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+    _INDEX.update({torch.int32: 32, torch.int64: 64})
+
+
+def _type(t) -> int:
+    if not _TYPES:
+        _learn_types()
+    code = _TYPES.get(t.dtype)
     if code is None:
         raise TypeError(f"{t.dtype}: float32, bfloat16 or float16 is wanted")
     return code
 
 
-def _same_device(*tensors):
+def _same_device(*tensors) -> int:
     """The tensors' one GPU; calls are made with it as the current device and, by default, on its current stream."""
-    dev = tensors[0].device
+    dev = tensors[0].get_device()
     for t in tensors:
-        if not t.is_cuda or t.device != dev:
+        if t.get_device() != dev or dev < 0:
             raise ValueError("device entry points take CUDA tensors of one device")
     return dev
 
 
-def _on(dev, stream) -> int:
+def _call(function, where: str, dev: int, stream, *args):
+    """function(*args, stream) on device `dev`; `stream`: a torch stream, or None for the device's current one"""
     import torch
-    return int((stream if stream is not None else torch.cuda.current_stream(dev)).cuda_stream)
-
-
-def _current(dev):
-    """a context in which `dev` is the current device"""
-    import contextlib
-
-    import torch
-    return contextlib.nullcontext() if torch.cuda.current_device() == dev.index else torch.cuda.device(dev)
+    s = int((stream if stream is not None else torch.cuda.current_stream(dev)).cuda_stream)
+    if torch.cuda.current_device() == dev:
+        code = function(*args, s)
+    else:
+        with torch.cuda.device(dev):
+            code = function(*args, s)
+    if code != OK:
+        raise FftspError(code, where)
 
 
 def _rows(t, width: int):
@@ -402,8 +413,9 @@ def _rows(t, width: int):
 
 
 def _tokens(t, count: int) -> int:
-    import torch
-    bits = {torch.int32: 32, torch.int64: 64}.get(t.dtype)
+    if not _INDEX:
+        _learn_types()
+    bits = _INDEX.get(t.dtype)
     if bits is None:
         raise TypeError(f"tokens are int32 or int64, got {t.dtype}")
     if not t.is_contiguous() or t.numel() != count:
@@ -418,9 +430,8 @@ def embedding(table, tokens, out, scale: float = 1.0, stream=None):
     tp, rows, ts = _rows(table, table.shape[-1])
     op, count, os_ = _rows(out, table.shape[-1])
     bits = _tokens(tokens, count)
-    with _current(dev):
-        _check(load().fftsp_embedding(tp, _type(table), rows, table.shape[-1], ts, tokens.data_ptr(), bits, count, scale,
-                                      op, _type(out), os_, _on(dev, stream)), "fftsp_embedding")
+    _call(load().fftsp_embedding, "fftsp_embedding", dev, stream, tp, _type(table), rows, table.shape[-1], ts,
+          tokens.data_ptr(), bits, count, scale, op, _type(out), os_)
 
 
 def workspace_bytes_embedding(rows: int, width: int, ntokens: int) -> int:
@@ -440,10 +451,9 @@ def embedding_gradient(out_grad, tokens, table_grad, workspace, scale: float = 1
         bp, brows, bs = _rows(base, width)
         if brows != rows or bs != ts or base.dtype != table_grad.dtype:
             raise ValueError("base has the shape, strides and type of table_grad")
-    with _current(dev):
-        _check(load().fftsp_embedding_gradient(gp, _type(out_grad), gs, tokens.data_ptr(), bits, count, scale, bp, tp,
-                                               _type(table_grad), rows, width, ts, _ptr(workspace), _nbytes(workspace),
-                                               _on(dev, stream)), "fftsp_embedding_gradient")
+    _call(load().fftsp_embedding_gradient, "fftsp_embedding_gradient", dev, stream, gp, _type(out_grad), gs,
+          tokens.data_ptr(), bits, count, scale, bp, tp, _type(table_grad), rows, width, ts, _ptr(workspace),
+          _nbytes(workspace))
 
 
 class Matrices:
@@ -484,10 +494,9 @@ def orthogonal(x, out, listing: Matrices, workspace, coefficients=None, eps: flo
     may be x).  coefficients: (a, b, c) of every step; None: five steps of (3.4445, -4.7750, 2.0315)."""
     dev = _same_device(x, out, workspace)
     co, steps = _coefficients(coefficients)  # kept alive until the call returns
-    with _current(dev):
-        _check(load().fftsp_orthogonal(_flat(x, listing, "x"), _type(x), _flat(out, listing, "out"), _type(out),
-                                       listing.array, listing.count, co, steps, eps, _ptr(workspace), _nbytes(workspace),
-                                       _on(dev, stream)), "fftsp_orthogonal")
+    _call(load().fftsp_orthogonal, "fftsp_orthogonal", dev, stream, _flat(x, listing, "x"), _type(x),
+          _flat(out, listing, "out"), _type(out), listing.array, listing.count, co, steps, eps, _ptr(workspace),
+          _nbytes(workspace))
 
 
 def orthogonal_step(grad, momentum, weights, listing: Matrices, workspace, lr: float, beta: float = 0.95,
@@ -505,13 +514,10 @@ def orthogonal_step(grad, momentum, weights, listing: Matrices, workspace, lr: f
         raise TypeError("weights_out has the type of weights")
     co, steps = _coefficients(coefficients)
     step = Step(lr, beta, weight_decay, eps, 1 if nesterov else 0, steps, co)
-    with _current(dev):
-        _check(load().fftsp_orthogonal_step(_flat(grad, listing, "grad"), _type(grad), _flat(momentum, listing, "momentum"),
-                                            _flat(momentum_out, listing, "momentum_out"),
-                                            _flat(weights, listing, "weights"),
-                                            _flat(weights_out, listing, "weights_out"), _type(weights), listing.array,
-                                            listing.count, C.byref(step), _ptr(workspace), _nbytes(workspace),
-                                            _on(dev, stream)), "fftsp_orthogonal_step")
+    _call(load().fftsp_orthogonal_step, "fftsp_orthogonal_step", dev, stream, _flat(grad, listing, "grad"), _type(grad),
+          _flat(momentum, listing, "momentum"), _flat(momentum_out, listing, "momentum_out"),
+          _flat(weights, listing, "weights"), _flat(weights_out, listing, "weights_out"), _type(weights), listing.array,
+          listing.count, C.byref(step), _ptr(workspace), _nbytes(workspace))
 
 
 def device_status(workspace) -> int:

@@ -87,7 +87,11 @@ CASES = [(1, 1, 1), (5, 3, 7), (1000, 64, 257), (100, 771, 4099), (9, 513, 5000)
          (70000, 128, 20000), (600, 2050, 4096), (1, 96, 12345)]
 
 
-@pytest.mark.parametrize("rows,width,count", CASES)
+# where the ways of summing and sorting change, and one place to either side
+EDGES = [(700, 72, n) for n in (63, 64, 65, 255, 257, 1023, 1024, 1025, 8191, 8192, 8193, 10240, 65537)]
+
+
+@pytest.mark.parametrize("rows,width,count", CASES + EDGES)
 @pytest.mark.parametrize("source,out", [("float32", "float32"), ("bfloat16", "float32"), ("float16", "bfloat16"),
                                         ("bfloat16", "bfloat16"), ("float32", "float16")])
 @pytest.mark.parametrize("base", ["none", "apart", "place"])
