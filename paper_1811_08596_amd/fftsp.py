@@ -360,20 +360,26 @@ F32, BF16, F16 = range(3)
 
 _TYPES: dict = {}   # torch's types as fftsp_type, filled at the first call (torch is not loaded at import)
 _INDEX: dict = {}
+_torch = None
 
 
-def _learn_types():
-    import torch
-    _TYPES.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
-    _INDEX.update({torch.int32: 32, torch.int64: 64})
+def _load_torch():
+    global _torch
+    if _torch is None:
+        import torch
+        _TYPES.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+        _INDEX.update({torch.int32: 32, torch.int64: 64})
+        _torch = torch
+    return _torch
 
 
 def _type(t) -> int:
-    if not _TYPES:
-        _learn_types()
     code = _TYPES.get(t.dtype)
     if code is None:
-        raise TypeError(f"{t.dtype}: float32, bfloat16 or float16 is wanted")
+        _load_torch()
+        code = _TYPES.get(t.dtype)
+        if code is None:
+            raise TypeError(f"{t.dtype}: float32, bfloat16 or float16 is wanted")
     return code
 
 
@@ -388,8 +394,8 @@ def _same_device(*tensors) -> int:
 
 def _call(function, where: str, dev: int, stream, *args):
     """function(*args, stream) on device `dev`; `stream`: a torch stream, or None for the device's current one"""
-    import torch
-    s = int((stream if stream is not None else torch.cuda.current_stream(dev)).cuda_stream)
+    torch = _load_torch()
+    s = (stream if stream is not None else torch.cuda.current_stream(dev)).cuda_stream
     if torch.cuda.current_device() == dev:
         code = function(*args, s)
     else:
@@ -402,19 +408,21 @@ def _call(function, where: str, dev: int, stream, *args):
 def _rows(t, width: int):
     """(data pointer, rows, distance of rows) of a tensor whose last axis holds `width` consecutive values; more than two
     axes have to be contiguous"""
-    if t.dim() != 2:
-        if t.dim() < 2 or not t.is_contiguous():
+    shape = t.shape
+    if len(shape) != 2:
+        if len(shape) < 2 or not t.is_contiguous():
             raise ValueError("rows are a 2-D tensor, or a contiguous one of more axes")
-        t = t.view(-1, t.shape[-1])
-    if t.shape[1] != width or (width > 1 and t.stride(1) != 1):
-        raise ValueError(f"rows of {width} consecutive values are wanted, got {tuple(t.shape)} with strides {t.stride()}")
-    stride = t.stride(0) if t.shape[0] > 1 else max(width, t.stride(0))
-    return t.data_ptr(), t.shape[0], stride
+        t = t.view(-1, shape[-1])
+        shape = t.shape
+    rows, values = shape
+    stride, one = t.stride()
+    if values != width or (width > 1 and one != 1):
+        raise ValueError(f"rows of {width} consecutive values are wanted, got {tuple(shape)} with strides {t.stride()}")
+    return t.data_ptr(), rows, stride if rows > 1 else max(width, stride)
 
 
 def _tokens(t, count: int) -> int:
-    if not _INDEX:
-        _learn_types()
+    _load_torch()
     bits = _INDEX.get(t.dtype)
     if bits is None:
         raise TypeError(f"tokens are int32 or int64, got {t.dtype}")
@@ -504,7 +512,7 @@ def orthogonal_step(grad, momentum, weights, listing: Matrices, workspace, lr: f
                     momentum_out=None, weights_out=None, stream=None):
     """M <- beta M + G; W <- (1 - lr weight_decay) W - lr gain O(G + beta M) for every matrix of `listing` in the flat
     arrays grad, momentum (float32) and weights; in place unless momentum_out, weights_out are given."""
-    import torch
+    torch = _load_torch()
     momentum_out = momentum if momentum_out is None else momentum_out
     weights_out = weights if weights_out is None else weights_out
     dev = _same_device(grad, momentum, weights, workspace, momentum_out, weights_out)
