@@ -395,6 +395,7 @@ struct ProductArgs {
     int phase;                   // X is x[phase & 1]
     int cls;
     uint32_t len;                // steps that a workgroup has at most
+    int local;                   // neighbouring workgroups' operands fit an XCD's L2
 };
 
 // Of a tile on the diagonal: the wave's blocks are above it, or what is above the diagonal for them is left out
@@ -609,9 +610,11 @@ __global__ void __launch_bounds__(S::kThreads, 2) k_product(ProductArgs g)
     extern __shared__ __align__(1024) uint8_t lds[];
     const Common& c = g.c;
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    // workgroups go round the eight XCDs: 32 tiles behind each other, which have operands in common, to each of them in turn
+    // Workgroups go round the eight XCDs.  32 tiles behind each other to each of them in turn where their operands, which they
+    // have in common, fit its L2 (eight matrices of 1024 x 1024: 41 us a launch instead of 48); elsewhere all XCDs then read other
+    // panels at a time (4096 x 9216: X X^T in 900 us instead of 620).
     uint32_t wg = blockIdx.x;
-    if ((wg | 255u) < gridDim.x) wg = (wg & ~255u) + (wg & 7u) * 32u + (wg >> 3 & 31u);
+    if (g.local && (wg | 255u) < gridDim.x) wg = (wg & ~255u) + (wg & 7u) * 32u + (wg >> 3 & 31u);
     uint32_t at, ti, tj;
     const Item it = c.items[find_item(c.starts + (size_t)(kProducts + g.cls) * c.count, c.count, wg, &at)];
     const uint32_t per = steps_of(it, WHAT), slices = (per + g.len - 1) / g.len;
@@ -903,7 +906,8 @@ __global__ void __launch_bounds__(kChainThreads, 2) k_chain(ChainArgs g)
 struct Share {
     int size;
     uint32_t len, workgroups;
-    double us;  // what it is thought to take
+    double us;   // what it is thought to take
+    bool local;  // neighbouring workgroups' operands fit an XCD's L2
 };
 struct Layout {
     size_t items, starts, sums, arrivals, partial, total;
@@ -945,8 +949,9 @@ uint64_t class_tiles(const MatrixSpan& m, bool chains, int cls, int size)
 
 // What a launch takes, in us: a step of a tile, what a workgroup does before and behind its steps, and for a sliced tile, putting
 // a part down and taking one up.  By tile size.
-constexpr double kStepUs[kSizes] = {0.12, 0.26, 1.09}, kEndsUs[kSizes] = {3.0, 5.0, 12.0}, kPutUs[kSizes] = {2.0, 3.0, 9.0}, kTakeUs[kSizes] = {1.0, 2.0, 8.0};
-constexpr uint32_t kUnits = 256;  // compute units
+constexpr double kStepUs[kSizes] = {0.12, 0.28, 1.09}, kEndsUs[kSizes] = {3.0, 5.0, 12.0}, kPutUs[kSizes] = {2.0, 3.0, 9.0}, kTakeUs[kSizes] = {1.0, 2.0, 8.0};
+constexpr uint32_t kUnits = 256;           // compute units
+constexpr uint64_t kLocalBytes = 8 << 20;  // of a matrix's operand that a launch goes through
 constexpr double kChainUs = 6.0, kChainStepUs = 5.0;
 
 Share share_of(const MatrixSpan* m, int count, bool chains, int cls, int sizes)
@@ -973,10 +978,15 @@ Share share_of(const MatrixSpan* m, int count, bool chains, int cls, int sizes)
             if (sliced > 0) us += std::ceil(sliced / kUnits) * kPutUs[size] + slices * kTakeUs[size];
             if (best.workgroups == 0 || us < least) {
                 least = us;
-                best = Share{size, len, (uint32_t)std::min(workgroups, 4e9), us};
+                best = Share{size, len, (uint32_t)std::min(workgroups, 4e9), us, false};
             }
             if (len == kLeastSteps) break;
         }
+    uint64_t bytes = 0;
+    for (int i = 0; i < count; ++i)
+        if (class_tiles(m[i], chains, cls, best.size))
+            bytes = std::max(bytes, (uint64_t)std::min(m[i].rows, m[i].cols) * 64u * std::min(class_steps(m[i], cls), best.len));
+    best.local = bytes <= kLocalBytes;
     return best;
 }
 
@@ -1105,6 +1115,7 @@ hipError_t launch_product(const char* name, ProductArgs g, const Layout& places,
     const Share& share = places.share[g.cls];
     if (share.workgroups == 0) return hipSuccess;
     g.len = share.len;
+    g.local = share.local;
     switch (share.size) {
         case 0: return launch_shared<Least, WHAT>(name, g, share.workgroups, s);
         case 1: return launch_shared<Small, WHAT>(name, g, share.workgroups, s);
