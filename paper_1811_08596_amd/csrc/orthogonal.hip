@@ -69,7 +69,7 @@ struct ItemTable {
 };
 
 // starts: [kKinds][matrices]
-__global__ void k_items(ItemTable t, Item* items, uint32_t* starts)
+__device__ __forceinline__ void put_items(const ItemTable& t, Item* items, uint32_t* starts)
 {
     const uint32_t i = threadIdx.x;
     if (i < t.count) {
@@ -77,6 +77,7 @@ __global__ void k_items(ItemTable t, Item* items, uint32_t* starts)
         for (int k = 0; k < kKinds; ++k) starts[(size_t)k * t.total + t.first + i] = t.start[i][k];
     }
 }
+__global__ void k_items(ItemTable t, Item* items, uint32_t* starts) { put_items(t, items, starts); }
 
 // the last matrix whose first workgroup is not behind `wg`, and how far behind it wg is
 __device__ __forceinline__ uint32_t find_item(const uint32_t* starts, uint32_t count, uint32_t wg, uint32_t* within)
@@ -184,11 +185,29 @@ __device__ __forceinline__ double norm_of_type(const Common& c, const Item& it, 
 {
     return c.step ? norm_part<T, true>(c, it, part) : norm_part<T, false>(c, it, part);
 }
-__global__ void __launch_bounds__(256) k_norm(Common c)
+// ARGUMENTS: the whole list is in the launch's arguments, and the first workgroup writes it down for the later launches
+template <bool ARGUMENTS>
+struct NormTable {
+};
+template <>
+struct NormTable<true> {
+    ItemTable t;
+};
+template <bool ARGUMENTS>
+__global__ void __launch_bounds__(256) k_norm(Common c, NormTable<ARGUMENTS> table)
 {
     __shared__ double sums[4];
-    uint32_t part;
-    const Item it = c.items[find_item(c.starts + (size_t)kNorm * c.count, c.count, blockIdx.x, &part)];
+    uint32_t part, id = 0;
+    if constexpr (ARGUMENTS) {
+        if (blockIdx.x == 0) put_items(table.t, const_cast<Item*>(c.items), const_cast<uint32_t*>(c.starts));
+        while (id + 1 < c.count && table.t.start[id + 1][kNorm] <= blockIdx.x) ++id;
+        part = blockIdx.x - table.t.start[id][kNorm];
+    } else {
+        id = find_item(c.starts + (size_t)kNorm * c.count, c.count, blockIdx.x, &part);
+    }
+    Item it;
+    if constexpr (ARGUMENTS) it = table.t.item[id];
+    else it = c.items[id];
     for (uint32_t i = blockIdx.x * 256u + threadIdx.x; i < c.most; i += gridDim.x * 256u) c.arrivals[i] = 0;
     double s = c.in_type == 0 ? norm_of_type<float>(c, it, part) : c.in_type == 1 ? norm_of_type<Bf16>(c, it, part) : norm_of_type<F16>(c, it, part);
     for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
@@ -617,7 +636,7 @@ __global__ void __launch_bounds__(S::kThreads, 2) k_product(ProductArgs g)
     if (g.local && (wg | 255u) < gridDim.x) wg = (wg & ~255u) + (wg & 7u) * 32u + (wg >> 3 & 31u);
     uint32_t at, ti, tj;
     const Item it = c.items[find_item(c.starts + (size_t)(kProducts + g.cls) * c.count, c.count, wg, &at)];
-    const uint32_t per = steps_of(it, WHAT), slices = (per + g.len - 1) / g.len;
+    const uint32_t per = steps_of(it, WHAT), slices = per <= g.len ? 1u : (per + g.len - 1) / g.len;
     const uint32_t nt = (it.n + S::kTile - 1) / S::kTile;
     uint32_t tiles = nt * (nt + 1) / 2;
     if (!symmetric(WHAT)) tiles = nt * ((it.m + S::kTile - 1) / S::kTile);
@@ -626,8 +645,13 @@ __global__ void __launch_bounds__(S::kThreads, 2) k_product(ProductArgs g)
         product = 1;
         at -= tiles * slices;
     }
-    const uint32_t slice = at / tiles, tile = at - slice * tiles;  // workgroups of one slice behind each other
-    const uint32_t first = (uint32_t)((uint64_t)per * slice / slices), steps = (uint32_t)((uint64_t)per * (slice + 1) / slices) - first;
+    uint32_t slice = 0, tile = at, first = 0, steps = per;
+    if (slices > 1) {  // workgroups of one slice behind each other
+        slice = at / tiles;
+        tile = at - slice * tiles;
+        first = per * slice / slices;  // per < 2^17, slices <= kMostSlices
+        steps = per * (slice + 1) / slices - first;
+    }
     if (symmetric(WHAT)) {  // row ti has ti + 1 tiles
         ti = (uint32_t)((sqrtf(8.f * (float)tile + 1.f) - 1.f) * 0.5f);
         while (ti * (ti + 1) / 2 > tile) --ti;
@@ -1266,17 +1290,6 @@ hipError_t launch_orthogonal(const OrthogonalArgs& a, const MatrixSpan* m, int c
     if (!step_bounds(a.coefficients, a.nsteps, places.phase_steps, &bounds)) return hipErrorInvalidValue;
     Item* items = reinterpret_cast<Item*>(ws + places.items);
     uint32_t* starts = reinterpret_cast<uint32_t*>(ws + places.starts);
-    ItemTable t{};
-    t.total = (uint32_t)count;
-    lay_out(m, count, a.nsteps, most, [&](int i, const Item& it, const uint32_t* begun) {
-        t.item[t.count] = it;
-        for (int k = 0; k < kKinds; ++k) t.start[t.count][k] = begun[k];
-        if (++t.count == kItemsPerLaunch || i + 1 == count) {
-            FFTSP_LAUNCH("orthogonal_list", k_items, dim3(1), dim3(64), 0, s, t, items, starts);
-            t.first += t.count;
-            t.count = 0;
-        }
-    });
     Common c{};
     c.in = a.in;
     c.in_type = a.in_type;
@@ -1300,7 +1313,22 @@ hipError_t launch_orthogonal(const OrthogonalArgs& a, const MatrixSpan* m, int c
     c.count = (uint32_t)count;
     c.most = places.most;
     c.lift = lift_for(bounds.x[0]);
-    FFTSP_LAUNCH("orthogonal_norm", k_norm, dim3(places.count[kNorm]), dim3(256), 0, s, c);
+    NormTable<true> list{};
+    ItemTable& t = list.t;
+    t.total = (uint32_t)count;
+    lay_out(m, count, a.nsteps, most, [&](int i, const Item& it, const uint32_t* begun) {
+        t.item[t.count] = it;
+        for (int k = 0; k < kKinds; ++k) t.start[t.count][k] = begun[k];
+        if (++t.count < kItemsPerLaunch && i + 1 < count) return;
+        if (count <= kItemsPerLaunch) {
+            FFTSP_LAUNCH("orthogonal_norm", k_norm<true>, dim3(places.count[kNorm]), dim3(256), 0, s, c, list);
+        } else {
+            FFTSP_LAUNCH("orthogonal_list", k_items, dim3(1), dim3(64), 0, s, t, items, starts);
+        }
+        t.first += t.count;
+        t.count = 0;
+    });
+    if (count > kItemsPerLaunch) FFTSP_LAUNCH("orthogonal_norm", k_norm<false>, dim3(places.count[kNorm]), dim3(256), 0, s, c, NormTable<false>{});
     FFTSP_LAUNCH("orthogonal_convert", k_convert, dim3(places.count[kConvert]), dim3(256), 0, s, c);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
