@@ -111,11 +111,10 @@ int run_orthogonal(const OrthogonalArgs& a, const fftsp_matrix* m, int count, vo
 {
     const MatrixSpan* spans = reinterpret_cast<const MatrixSpan*>(m);
     if (!ws || !aligned16(ws)) return FFTSP_EINVAL;
-    const size_t need = orthogonal_workspace(spans, count);
-    if (need == 0) return FFTSP_EUNSUPPORTED;
-    if (ws_bytes < need) return FFTSP_EWORKSPACE;
-    return launch_orthogonal(a, spans, count, static_cast<uint8_t*>(ws), reinterpret_cast<hipStream_t>(stream)) == hipSuccess ? FFTSP_OK
-                                                                                                                           : FFTSP_EHIP;
+    bool fits = false, enough = false;
+    const hipError_t e = launch_orthogonal(a, spans, count, static_cast<uint8_t*>(ws), ws_bytes, &fits, &enough, reinterpret_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return FFTSP_EHIP;
+    return !fits ? FFTSP_EUNSUPPORTED : !enough ? FFTSP_EWORKSPACE : FFTSP_OK;
 }
 
 // no exception leaves an entry point: the host's lists could not be allocated

@@ -114,6 +114,8 @@ struct MatrixSpan {  // fftsp_matrix
     uint32_t reserved;
 };
 size_t orthogonal_workspace(const MatrixSpan* m, int count);
-hipError_t launch_orthogonal(const OrthogonalArgs& a, const MatrixSpan* m, int count, uint8_t* ws, hipStream_t s);
+// *fits: the list's counts are within a launch's; *enough: so is the workspace.  Nothing is launched where one is false.
+hipError_t launch_orthogonal(const OrthogonalArgs& a, const MatrixSpan* m, int count, uint8_t* ws, size_t ws_bytes, bool* fits, bool* enough,
+                             hipStream_t s);
 
 }  // namespace fftsp

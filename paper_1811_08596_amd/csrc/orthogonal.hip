@@ -25,6 +25,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <vector>
 
 namespace fftsp {
 namespace {
@@ -936,8 +937,6 @@ struct Share {
 struct Layout {
     size_t items, starts, sums, arrivals, partial, total;
     uint32_t count[kKinds], most;
-    Share share[kClasses];
-    int phase_steps;
     bool fits;  // the counts are within 32 bits
 };
 
@@ -947,28 +946,28 @@ uint32_t norm_parts(const MatrixSpan& m)
     const uint64_t pieces = m.stride == m.cols ? ((uint64_t)m.rows * m.cols + kPiece - 1) / kPiece : (uint64_t)m.rows * ((m.cols + kPiece - 1) / kPiece);
     return (uint32_t)std::min<uint64_t>(kMostParts, (pieces + 1) / 2);
 }
-uint32_t class_steps(const MatrixSpan& m, int cls)
-{
-    const uint32_t n = std::min(m.rows, m.cols), w = std::max(m.rows, m.cols);
-    return ((cls == kGrams ? w : n) + 15) / 16;
-}
+// What a list's matrix has of every class: steps of a tile, and tiles by size.
+struct Work {
+    uint32_t steps[kClasses];
+    uint64_t tiles[kSizes][kClasses];
+    int chain;
+};
 // chains: every matrix of the list is short enough.  Beside longer ones, whose launches there are anyway, the short ones' tiles
 // cost nothing, and their chains would hold up the others.
-int chain_of(const MatrixSpan& m, bool chains)
+Work work_of(const MatrixSpan& m, bool chains)
 {
-    if (!chains) return 0;
-    return std::min(m.rows, m.cols) <= kChainGram && class_steps(m, kGrams) <= kChainGramSteps ? 2 : 1;
-}
-uint64_t class_tiles(const MatrixSpan& m, bool chains, int cls, int size)
-{
-    const uint64_t t = kTileOf[size], nt = (std::min(m.rows, m.cols) + t - 1) / t, mt = (std::max(m.rows, m.cols) + t - 1) / t;
-    const int chain = chain_of(m, chains);
-    switch (cls) {
-        case kGrams: return chain == 2 ? 0 : nt * (nt + 1) / 2;
-        case kSingles: return chain ? 0 : nt * (nt + 1) / 2;
-        case kPairs: return chain ? 0 : nt * (nt + 1);
-        default: return nt * mt;
+    Work w{};
+    const uint32_t n = std::min(m.rows, m.cols), wide = std::max(m.rows, m.cols), nsteps = (n + 15) / 16, msteps = (wide + 15) / 16;
+    w.chain = !chains ? 0 : n <= kChainGram && msteps <= kChainGramSteps ? 2 : 1;
+    for (int cls = 0; cls < kClasses; ++cls) w.steps[cls] = cls == kGrams ? msteps : nsteps;
+    for (int size = 0; size < kSizes; ++size) {
+        const uint64_t t = kTileOf[size], nt = (n + t - 1) / t, mt = (wide + t - 1) / t, half = nt * (nt + 1) / 2;
+        w.tiles[size][kGrams] = w.chain == 2 ? 0 : half;
+        w.tiles[size][kSingles] = w.chain ? 0 : half;
+        w.tiles[size][kPairs] = w.chain ? 0 : 2 * half;
+        w.tiles[size][kWides] = nt * mt;
     }
+    return w;
 }
 
 // What a launch takes, in us: a step of a tile, what a workgroup does before and behind its steps, and for a sliced tile, putting
@@ -978,38 +977,38 @@ constexpr uint32_t kUnits = 256;           // compute units
 constexpr uint64_t kLocalBytes = 8 << 20;  // of a matrix's operand that a launch goes through
 constexpr double kChainUs = 6.0, kChainStepUs = 5.0;
 
-Share share_of(const MatrixSpan* m, int count, bool chains, int cls, int sizes)
+Share share_of(const std::vector<Work>& work, const MatrixSpan* m, int cls, int sizes)
 {
     Share best{};
     double least = 0.0;
     uint32_t longest = 0;
-    for (int i = 0; i < count; ++i)
-        if (class_tiles(m[i], chains, cls, 0)) longest = std::max(longest, class_steps(m[i], cls));
-    for (int size = 0; size < sizes; ++size)
-        for (uint32_t slices = 1; slices <= kMostSlices && longest; ++slices) {
-            const uint32_t len = std::max(kLeastSteps, (longest + slices - 1) / slices);
+    for (const Work& w : work)
+        if (w.tiles[0][cls]) longest = std::max(longest, w.steps[cls]);
+    for (int size = 0; size < sizes && longest; ++size)
+        for (uint32_t slices = 1; slices <= kMostSlices; slices += slices < 4 ? 1 : slices / 2) {  // 1 2 3 4 6 9 13 19 28 42 63
+            const uint32_t len = std::max(std::min(kLeastSteps, longest), (longest + slices - 1) / slices);
             double workgroups = 0, steps = 0, sliced = 0;
-            for (int i = 0; i < count; ++i) {
-                const double tiles = (double)class_tiles(m[i], chains, cls, size);
-                const uint32_t per = class_steps(m[i], cls), s = (per + len - 1) / len;
+            for (const Work& w : work) {
+                const double tiles = (double)w.tiles[size][cls];
+                const uint32_t per = w.steps[cls], s = per <= len ? 1 : (per + len - 1) / len;
                 workgroups += tiles * s;
                 steps += tiles * per;
                 if (s > 1) sliced += tiles * s;
             }
             // every compute unit has as many, or the work is even but for the last one's
-            const double one = std::min(len, longest) * kStepUs[size] + kEndsUs[size];
+            const double one = len * kStepUs[size] + kEndsUs[size];
             double us = std::min(std::ceil(workgroups / kUnits) * one, (steps * kStepUs[size] + workgroups * kEndsUs[size]) / kUnits + one);
             if (sliced > 0) us += std::ceil(sliced / kUnits) * kPutUs[size] + slices * kTakeUs[size];
             if (best.workgroups == 0 || us < least) {
                 least = us;
                 best = Share{size, len, (uint32_t)std::min(workgroups, 4e9), us, false};
             }
-            if (len == kLeastSteps) break;
+            if (len <= kLeastSteps) break;
         }
     uint64_t bytes = 0;
-    for (int i = 0; i < count; ++i)
-        if (class_tiles(m[i], chains, cls, best.size))
-            bytes = std::max(bytes, (uint64_t)std::min(m[i].rows, m[i].cols) * 64u * std::min(class_steps(m[i], cls), best.len));
+    for (size_t i = 0; i < work.size(); ++i)
+        if (work[i].tiles[0][cls])
+            bytes = std::max(bytes, (uint64_t)std::min(m[i].rows, m[i].cols) * 64u * std::min(work[i].steps[cls], best.len));
     best.local = bytes <= kLocalBytes;
     return best;
 }
@@ -1039,26 +1038,42 @@ int phase_steps_of(const Share* share, bool chains, int nsteps, int most)
     return best;
 }
 
+// How a list is taken: everything that its shapes decide.
+struct Plan {
+    std::vector<Work> work;
+    Share share[kClasses];
+    uint32_t room;  // rows and columns that there is room for are multiples of this
+    int phase_steps;
+};
+Plan plan_of(const MatrixSpan* m, int count, int nsteps, int most_phase)
+{
+    Plan p{};
+    uint32_t highest = 0;
+    for (int i = 0; i < count; ++i) highest = std::max(highest, std::min(m[i].rows, m[i].cols));
+    const bool chains = highest <= kChainMost;
+    p.work.reserve((size_t)count);
+    for (int i = 0; i < count; ++i) p.work.push_back(work_of(m[i], chains));
+    const int sizes = highest > Large::kTile ? kSizes : kSizes - 1;
+    p.room = kTileOf[sizes - 1];
+    for (int cls = 0; cls < kClasses; ++cls) p.share[cls] = share_of(p.work, m, cls, sizes);
+    p.phase_steps = phase_steps_of(p.share, chains, nsteps, most_phase);
+    return p;
+}
+
 // the matrices' places; each(i, item, units of the kinds before it)
 template <typename Each>
-Layout lay_out(const MatrixSpan* m, int count, int nsteps, int most_phase, Each&& each)
+Layout lay_out(const MatrixSpan* m, int count, const Plan& plan, Each&& each)
 {
     Layout l{};
     uint64_t sum[kKinds] = {}, sums = 0;
-    uint32_t highest = 0;
-    for (int i = 0; i < count; ++i) {
-        sums += norm_parts(m[i]);
-        highest = std::max(highest, std::min(m[i].rows, m[i].cols));
-    }
-    const bool chains = highest <= kChainMost;
-    const int sizes = highest > Large::kTile ? kSizes : kSizes - 1;
-    const uint32_t room = kTileOf[sizes - 1];
-    for (int cls = 0; cls < kClasses; ++cls) l.share[cls] = share_of(m, count, chains, cls, sizes);
+    for (int i = 0; i < count; ++i) sums += norm_parts(m[i]);
     size_t off = 0;
     l.items = off;  off = align256(off + (size_t)count * sizeof(Item));
     l.starts = off; off = align256(off + (size_t)count * kKinds * 4);
     l.sums = off;   off = align256(off + sums * 8);
+    bool sliced[kClasses] = {};
     for (int i = 0; i < count; ++i) {
+        const Work& w = plan.work[(size_t)i];
         Item it{};
         it.at = m[i].offset;
         it.stride = m[i].stride;
@@ -1066,11 +1081,11 @@ Layout lay_out(const MatrixSpan* m, int count, int nsteps, int most_phase, Each&
         it.cols = m[i].cols;
         it.n = std::min(it.rows, it.cols);
         it.m = std::max(it.rows, it.cols);
-        const uint32_t np = (it.n + room - 1) / room * room, mp = (it.m + room - 1) / room * room;
+        const uint32_t np = (it.n + plan.room - 1) / plan.room * plan.room, mp = (it.m + plan.room - 1) / plan.room * plan.room;
         it.nf = np / 16;
         it.mf = mp / 16;
         it.gain = m[i].gain;
-        it.chain = (uint32_t)chain_of(m[i], chains);
+        it.chain = (uint32_t)w.chain;
         const size_t x = (size_t)np * mp * 4;
         for (int k = 0; k < 2; ++k) {
             it.x[k] = off;  off += x;
@@ -1085,8 +1100,11 @@ Layout lay_out(const MatrixSpan* m, int count, int nsteps, int most_phase, Each&
         units[kConvert] = (uint64_t)((it.n + 63) / 64) * ((it.m + 63) / 64);
         units[kChain] = it.chain != 0;
         for (int cls = 0; cls < kClasses; ++cls) {
-            const Share& s = l.share[cls];
-            if (s.workgroups) units[kProducts + cls] = class_tiles(m[i], chains, cls, s.size) * ((class_steps(m[i], cls) + s.len - 1) / s.len);
+            const Share& s = plan.share[cls];
+            if (!s.workgroups) continue;
+            const uint32_t slices = (w.steps[cls] + s.len - 1) / s.len;
+            units[kProducts + cls] = w.tiles[s.size][cls] * slices;
+            sliced[cls] = sliced[cls] || (slices > 1 && w.tiles[s.size][cls]);
         }
         each(i, it, l.count);
         for (int k = 0; k < kKinds; ++k) l.count[k] = (uint32_t)(sum[k] += units[k]);
@@ -1095,14 +1113,10 @@ Layout lay_out(const MatrixSpan* m, int count, int nsteps, int most_phase, Each&
     for (int k = 0; k < kKinds; ++k) l.fits = l.fits && sum[k] < (uint64_t)1 << 22;  // of 512 threads: within a launch's 2^32
     size_t partial = 0;
     for (int cls = 0; cls < kClasses; ++cls) {
-        const Share& s = l.share[cls];
-        bool sliced = false;
-        for (int i = 0; i < count; ++i) sliced = sliced || (class_tiles(m[i], chains, cls, s.size) && class_steps(m[i], cls) > s.len);
-        if (!sliced) continue;
-        l.most = std::max(l.most, s.workgroups);
-        partial = std::max(partial, (size_t)s.workgroups * kTileBytesOf[s.size]);
+        if (!sliced[cls]) continue;
+        l.most = std::max(l.most, l.count[kProducts + cls]);
+        partial = std::max(partial, (size_t)l.count[kProducts + cls] * kTileBytesOf[plan.share[cls].size]);
     }
-    l.phase_steps = phase_steps_of(l.share, l.count[kChain] != 0, nsteps, most_phase);
     l.arrivals = align256(off);
     l.partial = align256(l.arrivals + (size_t)l.most * 4);
     l.total = l.partial + partial;
@@ -1133,17 +1147,18 @@ hipError_t launch_shared(const char* name, const ProductArgs& g, uint32_t workgr
     return hipGetLastError();
 }
 template <int WHAT>
-hipError_t launch_product(const char* name, ProductArgs g, const Layout& places, hipStream_t s)
+hipError_t launch_product(const char* name, ProductArgs g, const Plan& plan, const Layout& places, hipStream_t s)
 {
     g.cls = WHAT == kGram ? kGrams : !symmetric(WHAT) ? kWides : WHAT == kTimes && g.products == 2 ? kPairs : kSingles;
-    const Share& share = places.share[g.cls];
-    if (share.workgroups == 0) return hipSuccess;
+    const Share& share = plan.share[g.cls];
+    const uint32_t workgroups = places.count[kProducts + g.cls];
+    if (workgroups == 0) return hipSuccess;
     g.len = share.len;
     g.local = share.local;
     switch (share.size) {
-        case 0: return launch_shared<Least, WHAT>(name, g, share.workgroups, s);
-        case 1: return launch_shared<Small, WHAT>(name, g, share.workgroups, s);
-        default: return launch_shared<Large, WHAT>(name, g, share.workgroups, s);
+        case 0: return launch_shared<Least, WHAT>(name, g, workgroups, s);
+        case 1: return launch_shared<Small, WHAT>(name, g, workgroups, s);
+        default: return launch_shared<Large, WHAT>(name, g, workgroups, s);
     }
 }
 
@@ -1156,7 +1171,7 @@ float lift_for(double bound)
     return (float)std::ldexp(1.0, e);
 }
 
-hipError_t launch_steps(const Common& c, const OrthogonalArgs& a, const StepBounds& b, const Layout& places, hipStream_t s)
+hipError_t launch_steps(const Common& c, const OrthogonalArgs& a, const StepBounds& b, const Plan& plan, const Layout& places, hipStream_t s)
 {
     hipError_t e = hipSuccess;
     int step = 0;
@@ -1172,7 +1187,7 @@ hipError_t launch_steps(const Common& c, const OrthogonalArgs& a, const StepBoun
         g.out[0] = kA;
         float la = lift_for(b.a[step]), lq = 1.f;
         chain.gram = g.scale[0] = la / (lx * lx);
-        e = launch_product<kGram>("orthogonal_gram", g, places, s);
+        e = launch_product<kGram>("orthogonal_gram", g, plan, places, s);
         int q = kQ0;
         for (const int first = step; step < b.end[phase] && e == hipSuccess; ++step) {
             ChainStep& st = chain.step[chain.steps++];
@@ -1184,7 +1199,7 @@ hipError_t launch_steps(const Common& c, const OrthogonalArgs& a, const StepBoun
             st.poly = g.scale[0] = a.coefficients[3 * step + 2] * (lp / (la * la));
             g.left[0] = g.right[0] = kA;
             g.out[0] = p;
-            e = launch_product<kPoly>("orthogonal_poly", g, places, s);
+            e = launch_product<kPoly>("orthogonal_poly", g, plan, places, s);
             if (e != hipSuccess) break;
             const bool again = step + 1 < b.end[phase];
             const float lt = lift_for(b.t[step]);
@@ -1207,7 +1222,7 @@ hipError_t launch_steps(const Common& c, const OrthogonalArgs& a, const StepBoun
                 lq = lp;
             }
             g.products = k;
-            if (k) e = launch_product<kTimes>("orthogonal_times", g, places, s);
+            if (k) e = launch_product<kTimes>("orthogonal_times", g, plan, places, s);
             if (again && e == hipSuccess) {  // A <- T P
                 const float next = lift_for(b.a[step + 1]);
                 g.products = 1;
@@ -1216,7 +1231,7 @@ hipError_t launch_steps(const Common& c, const OrthogonalArgs& a, const StepBoun
                 st.a = g.scale[0] = next / (lt * lp);
                 la = next;
                 g.out[0] = kA;
-                e = launch_product<kTimes>("orthogonal_times", g, places, s);
+                e = launch_product<kTimes>("orthogonal_times", g, plan, places, s);
             }
         }
         if (e == hipSuccess && places.count[kChain]) {
@@ -1229,10 +1244,10 @@ hipError_t launch_steps(const Common& c, const OrthogonalArgs& a, const StepBoun
         g.left[0] = q;
         if (phase + 1 < b.phases) {
             g.scale[0] = lift_for(b.x[phase + 1]) / (lq * lx);
-            e = launch_product<kApply>("orthogonal_apply", g, places, s);
+            e = launch_product<kApply>("orthogonal_apply", g, plan, places, s);
         } else {
             g.scale[0] = 1.f / (lq * lx);
-            e = launch_product<kLast>("orthogonal_last", g, places, s);
+            e = launch_product<kLast>("orthogonal_last", g, plan, places, s);
         }
     }
     return e;
@@ -1278,16 +1293,21 @@ bool step_bounds(const float* coefficients, int nsteps, int phase_steps, StepBou
 
 size_t orthogonal_workspace(const MatrixSpan* m, int count)
 {
-    const Layout l = lay_out(m, count, 1, 1, [](int, const Item&, const uint32_t*) {});
-    return count && l.fits ? l.total : 0;
+    if (!count) return 0;
+    const Layout l = lay_out(m, count, plan_of(m, count, 1, 1), [](int, const Item&, const uint32_t*) {});
+    return l.fits ? l.total : 0;
 }
 
-hipError_t launch_orthogonal(const OrthogonalArgs& a, const MatrixSpan* m, int count, uint8_t* ws, hipStream_t s)
+hipError_t launch_orthogonal(const OrthogonalArgs& a, const MatrixSpan* m, int count, uint8_t* ws, size_t ws_bytes, bool* fits, bool* enough,
+                             hipStream_t s)
 {
-    const int most = a.out_type == 0 ? kPhaseMost32 : kPhaseMost;
-    const Layout places = lay_out(m, count, a.nsteps, most, [](int, const Item&, const uint32_t*) {});
+    const Plan plan = plan_of(m, count, a.nsteps, a.out_type == 0 ? kPhaseMost32 : kPhaseMost);
+    const Layout places = lay_out(m, count, plan, [](int, const Item&, const uint32_t*) {});
     StepBounds bounds;
-    if (!step_bounds(a.coefficients, a.nsteps, places.phase_steps, &bounds)) return hipErrorInvalidValue;
+    if (!step_bounds(a.coefficients, a.nsteps, plan.phase_steps, &bounds)) return hipErrorInvalidValue;
+    *fits = places.fits;
+    *enough = ws_bytes >= places.total;
+    if (!*fits || !*enough) return hipSuccess;
     Item* items = reinterpret_cast<Item*>(ws + places.items);
     uint32_t* starts = reinterpret_cast<uint32_t*>(ws + places.starts);
     Common c{};
@@ -1316,7 +1336,7 @@ hipError_t launch_orthogonal(const OrthogonalArgs& a, const MatrixSpan* m, int c
     NormTable<true> list{};
     ItemTable& t = list.t;
     t.total = (uint32_t)count;
-    lay_out(m, count, a.nsteps, most, [&](int i, const Item& it, const uint32_t* begun) {
+    lay_out(m, count, plan, [&](int i, const Item& it, const uint32_t* begun) {
         t.item[t.count] = it;
         for (int k = 0; k < kKinds; ++k) t.start[t.count][k] = begun[k];
         if (++t.count < kItemsPerLaunch && i + 1 < count) return;
@@ -1332,7 +1352,7 @@ hipError_t launch_orthogonal(const OrthogonalArgs& a, const MatrixSpan* m, int c
     FFTSP_LAUNCH("orthogonal_convert", k_convert, dim3(places.count[kConvert]), dim3(256), 0, s, c);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    return launch_steps(c, a, bounds, places, s);
+    return launch_steps(c, a, bounds, plan, places, s);
 }
 
 }  // namespace fftsp
