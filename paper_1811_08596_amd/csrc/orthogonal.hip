@@ -294,6 +294,7 @@ struct Shape {
     static constexpr uint32_t kTurn = 32 * 36 * 4;                      // a wave's part of LDS in the epilogue
     static constexpr uint32_t kLds = std::max(kStage * STAGES, kTurn * kWaves);
     static constexpr uint32_t kTileBytes = kTile * kTile * 4;
+    static constexpr bool kSliced = kTile < 256;  // putting down and taking up parts of 256 KB costs more than it gains
     static_assert(kLeft == kRight && (kLeft + kRight) * 2 % kWaves == 0 && kPieces * (STAGES - 2) < 64 && STAGES >= 3, "");
 };
 using Least = Shape<2, 2, 1, 1, 8>;  // 64 x 64
@@ -301,6 +302,7 @@ using Small = Shape<2, 2, 2, 2, 5>;  // 128 x 128, two workgroups to a compute u
 using Large = Shape<2, 4, 4, 2, 4>;  // 256 x 256, one
 constexpr int kSizes = 3;
 constexpr uint32_t kTileOf[kSizes] = {Least::kTile, Small::kTile, Large::kTile}, kTileBytesOf[kSizes] = {Least::kTileBytes, Small::kTileBytes, Large::kTileBytes};
+static_assert(Least::kSliced && Small::kSliced && !Large::kSliced, "the last size is not sliced");
 
 template <int N>
 __device__ __forceinline__ void arrived()  // all but the wave's last N pieces; then everybody's
@@ -637,7 +639,7 @@ __global__ void __launch_bounds__(S::kThreads, 2) k_product(ProductArgs g)
     if (g.local && (wg | 255u) < gridDim.x) wg = (wg & ~255u) + (wg & 7u) * 32u + (wg >> 3 & 31u);
     uint32_t at, ti, tj;
     const Item it = c.items[find_item(c.starts + (size_t)(kProducts + g.cls) * c.count, c.count, wg, &at)];
-    const uint32_t per = steps_of(it, WHAT), slices = per <= g.len ? 1u : (per + g.len - 1) / g.len;
+    const uint32_t per = steps_of(it, WHAT), slices = !S::kSliced || per <= g.len ? 1u : (per + g.len - 1) / g.len;
     const uint32_t nt = (it.n + S::kTile - 1) / S::kTile;
     uint32_t tiles = nt * (nt + 1) / 2;
     if (!symmetric(WHAT)) tiles = nt * ((it.m + S::kTile - 1) / S::kTile);
@@ -647,7 +649,7 @@ __global__ void __launch_bounds__(S::kThreads, 2) k_product(ProductArgs g)
         at -= tiles * slices;
     }
     uint32_t slice = 0, tile = at, first = 0, steps = per;
-    if (slices > 1) {  // workgroups of one slice behind each other
+    if (S::kSliced && slices > 1) {  // workgroups of one slice behind each other
         slice = at / tiles;
         tile = at - slice * tiles;
         first = per * slice / slices;  // per < 2^17, slices <= kMostSlices
@@ -666,7 +668,7 @@ __global__ void __launch_bounds__(S::kThreads, 2) k_product(ProductArgs g)
     tj = __builtin_amdgcn_readfirstlane(tj);
     Accumulators<S> acc;
     multiply_tile<S, WHAT>(g, it, product, ti, tj, first, steps, acc, lds, wave, lane);
-    if (slices > 1) {
+    if (S::kSliced && slices > 1) {
         const uint32_t wg0 = wg - slice * tiles;
         auto part = [&](uint32_t s) { return reinterpret_cast<uint64_t*>(c.partial + (uint64_t)(wg0 + s * tiles) * S::kTileBytes) + threadIdx.x; };
         uint64_t* dst = part(slice);
@@ -972,7 +974,7 @@ Work work_of(const MatrixSpan& m, bool chains)
 
 // What a launch takes, in us: a step of a tile, what a workgroup does before and behind its steps, and for a sliced tile, putting
 // a part down and taking one up.  By tile size.
-constexpr double kStepUs[kSizes] = {0.12, 0.28, 1.09}, kEndsUs[kSizes] = {3.0, 5.0, 12.0}, kPutUs[kSizes] = {2.0, 3.0, 9.0}, kTakeUs[kSizes] = {1.0, 2.0, 8.0};
+constexpr double kStepUs[kSizes] = {0.12, 0.28, 1.09}, kEndsUs[kSizes] = {3.0, 5.0, 12.0}, kPutUs[kSizes - 1] = {2.0, 3.0}, kTakeUs[kSizes - 1] = {1.0, 2.0};
 constexpr uint32_t kUnits = 256;           // compute units
 constexpr uint64_t kLocalBytes = 8 << 20;  // of a matrix's operand that a launch goes through
 constexpr double kChainUs = 6.0, kChainStepUs = 5.0;
@@ -1003,7 +1005,7 @@ Share share_of(const std::vector<Work>& work, const MatrixSpan* m, int cls, int 
                 least = us;
                 best = Share{size, len, (uint32_t)std::min(workgroups, 4e9), us, false};
             }
-            if (len <= kLeastSteps) break;
+            if (len <= kLeastSteps || size == kSizes - 1) break;
         }
     uint64_t bytes = 0;
     for (size_t i = 0; i < work.size(); ++i)

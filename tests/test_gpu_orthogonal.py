@@ -20,6 +20,20 @@ def dev():
     return Device()
 
 
+def largest(torch, gram):
+    """its largest eigenvalue: exactly for small matrices, else by forty products with a vector, and a tenth more"""
+    if float(gram.abs().max()) == 0:
+        return 0.0
+    if gram.shape[0] <= 400:
+        return float(torch.linalg.matrix_norm(gram, 2))
+    v = torch.ones(gram.shape[0], 1, dtype=gram.dtype, device=gram.device)
+    for i in range(40):
+        v = gram @ v
+        size = float(torch.linalg.vector_norm(v))
+        v = v / size
+    return 1.1 * size
+
+
 def exact(torch, g, coefficients=DEFAULT, eps=1e-7):
     """(orthogonalised g in 64 bits, bound of the error's 2-norm)"""
     u = 2.0 ** -24
@@ -33,7 +47,7 @@ def exact(torch, g, coefficients=DEFAULT, eps=1e-7):
     e = u * (3 + 2 * np.sqrt(max(x.shape) / 16))
     for a, b, c in [[float(np.float32(v)) for v in abc] for abc in coefficients]:
         gram = x @ x.t()
-        top = float(torch.linalg.matrix_norm(gram, 2)) if float(gram.abs().max()) > 0 else 0.0
+        top = largest(torch, gram)
         size = float(torch.linalg.vector_norm(x))
         x = a * x + (b * gram + c * (gram @ gram)) @ x
         bound = bound * max(abs(a), 1.0) + e * size * (abs(a) + 2 * abs(b) * top + 3 * abs(c) * top * top) + u * float(torch.linalg.vector_norm(x))
@@ -107,6 +121,56 @@ def test_orthogonal(dev, name, source, out):
         place = x.clone()
         f.orthogonal(place, place, listing, ws)
         assert torch.equal(place[~rest], got[~rest])
+
+
+# tiles of 256 of every kind of product; rows so long that their sums are taken in slices; wide products in slices; many of one size
+LARGE = {
+    "four": [(2560, 2600)] * 4,
+    "two": [(4100, 2570), (2560, 2600)],
+    "long": [(300, 20000), (20003, 190)],
+    "deep": [(1024, 1030)],
+    "eight": [(1024, 1024)] * 8,
+}
+
+
+@pytest.mark.parametrize("name", list(LARGE))
+@pytest.mark.parametrize("kind", ["float32", "bfloat16"])
+def test_large(dev, name, kind):
+    torch, f = dev.torch, dev.f
+    shapes = LARGE[name]
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    listing, total, ms = lay(torch, f, shapes, [1.0] * len(shapes))
+    x = torch.zeros(total, device="cuda", dtype=getattr(torch, kind))
+    for m in ms:
+        view(torch, x, m).copy_(matrix_like(torch, gen, m.rows, m.cols))
+    got = torch.full((total,), float("nan"), device="cuda", dtype=x.dtype)
+    ws = dev.workspace(f.workspace_bytes_orthogonal(listing))
+    f.orthogonal(x, got, listing, ws)
+    half = torch.finfo(got.dtype).eps / 2
+    for m in ms:
+        want, bound = exact(torch, view(torch, x, m))
+        size = float(torch.linalg.vector_norm(want))
+        err = float(torch.linalg.vector_norm(view(torch, got, m).double() - want))
+        assert err <= bound + half * 1.001 * size, (m.rows, m.cols, err, bound)
+        # far inside that bound, which adds up the worst of every step: what binary32 products give
+        assert err <= (2e-5 + half) * size, (m.rows, m.cols, err / size)
+    again = torch.full_like(got, 1.0)
+    f.orthogonal(x, again, listing, ws)
+    assert torch.equal(again[:ms[-1].offset], got[:ms[-1].offset])
+
+
+def test_offsets_past_32_bits(dev):
+    torch, f = dev.torch, dev.f
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    at = (1 << 32) + 5
+    m = f.Matrix(at, 70, 40, (1 << 20) + 3)
+    listing = f.matrices([m])
+    x = torch.zeros(listing.end, device="cuda", dtype=torch.bfloat16)
+    view(torch, x, m).copy_(torch.randn(70, 40, device="cuda", generator=gen))
+    want, bound = exact(torch, view(torch, x, m))
+    f.orthogonal(x, x, listing, dev.workspace(f.workspace_bytes_orthogonal(listing)))
+    err = float(torch.linalg.vector_norm(view(torch, x, m).double() - want))
+    assert err <= bound + 2.0 ** -8 * 1.001 * float(torch.linalg.vector_norm(want))
 
 
 def test_ranks_sizes_and_zeros(dev):
