@@ -63,6 +63,7 @@ __device__ __forceinline__ uint64_t by_rows(const Item& it, int phase) { return 
 __device__ __forceinline__ uint64_t by_columns(const Item& it, int phase) { return phase & 1 ? it.xt[1] : it.xt[0]; }
 
 constexpr int kItemsPerLaunch = 24;
+static_assert(kItemsPerLaunch <= 64, "a lane each");
 struct ItemTable {
     Item item[kItemsPerLaunch];
     uint32_t start[kItemsPerLaunch][kKinds];
@@ -201,8 +202,9 @@ __global__ void __launch_bounds__(256) k_norm(Common c, NormTable<ARGUMENTS> tab
     uint32_t part, id = 0;
     if constexpr (ARGUMENTS) {
         if (blockIdx.x == 0) put_items(table.t, const_cast<Item*>(c.items), const_cast<uint32_t*>(c.starts));
-        while (id + 1 < c.count && table.t.start[id + 1][kNorm] <= blockIdx.x) ++id;
-        part = blockIdx.x - table.t.start[id][kNorm];
+        const uint32_t lane = threadIdx.x & 63u, v = lane < c.count ? table.t.start[lane][kNorm] : 0xFFFFFFFFu;
+        id = 63u - (uint32_t)__builtin_clzll(__ballot(v <= blockIdx.x));
+        part = blockIdx.x - (uint32_t)__builtin_amdgcn_readlane((int)v, (int)id);
     } else {
         id = find_item(c.starts + (size_t)kNorm * c.count, c.count, blockIdx.x, &part);
     }
@@ -224,6 +226,26 @@ __device__ __forceinline__ void split(float v, _Float16* hi, _Float16* lo)
 }
 
 // ---- U / (|U|_F + eps) as fragments, by rows and by columns: a workgroup per 64 x 64 values ----
+// A thread's values: four of rows tid / 16 + 16 q of the caller's array, which are on their way while the norm is added up
+template <typename T>
+__device__ __forceinline__ void convert_load(const Common& c, const Item& it, uint32_t row, uint32_t col, float (&v)[4][4])
+{
+    float m[4][4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const uint32_t r = row + 16u * q, n = r < it.rows && col < it.cols ? min(4u, it.cols - col) : 0u;
+        const uint64_t at = it.at + (uint64_t)r * it.stride + col;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[q][e] = m[q][e] = 0.f;
+        if (n) load_some<T>(static_cast<const T*>(c.in) + at, n, v[q]);
+        if (n && c.step) load_some<float>(c.momentum_out + at, n, m[q]);
+    }
+    if (c.step)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[q][e] = c.nesterov ? fmaf(c.beta, m[q][e], v[q][e]) : m[q][e];
+}
 __global__ void __launch_bounds__(256) k_convert(Common c)
 {
     __shared__ float tile[64][65];
@@ -231,33 +253,31 @@ __global__ void __launch_bounds__(256) k_convert(Common c)
     uint32_t at;
     const uint32_t id = find_item(c.starts + (size_t)kConvert * c.count, c.count, blockIdx.x, &at);
     const Item it = c.items[id];
-    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
-    double s = 0.0;
     const uint32_t first_part = c.starts[(size_t)kNorm * c.count + id];
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
+    // tile (tn, tm) of the iteration's n x m matrix
+    const uint32_t across = (it.m + 63u) / 64u, tn = at / across, tm = at - tn * across;
+    const bool t = tall(it);
+    const uint32_t slow = tid >> 4, fast = (tid & 15u) * 4u;
+    const uint32_t row = (t ? tm : tn) * 64u + slow, col = (t ? tn : tm) * 64u + fast;
+    float v[4][4];
+    if (c.in_type == 0) convert_load<float>(c, it, row, col, v);
+    else if (c.in_type == 1) convert_load<Bf16>(c, it, row, col, v);
+    else convert_load<F16>(c, it, row, col, v);
+    double s = 0.0;
     for (uint32_t i = tid; i < it.parts; i += 256) s += c.sums[first_part + i];
     for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
     if (lane == 0) sums[wave] = s;
     __syncthreads();
     const double norm = sqrt((sums[0] + sums[1]) + (sums[2] + sums[3])) + (double)c.eps;
     const double factor = norm > 0.0 ? (double)c.lift / norm : 0.0;
-    // tile (tn, tm) of the iteration's n x m matrix
-    const uint32_t across = (it.m + 63u) / 64u, tn = at / across, tm = at - tn * across;
-    for (uint32_t i = tid; i < 64 * 64; i += 256) {
-        // consecutive lanes along the caller's rows
-        const uint32_t slow = i >> 6, fast = i & 63u;
-        const uint32_t n = tn * 64 + (tall(it) ? fast : slow), m = tm * 64 + (tall(it) ? slow : fast);
-        float v = 0.f;
-        if (n < it.n && m < it.m) {
-            const uint64_t e = it.at + (tall(it) ? (uint64_t)m * it.stride + n : (uint64_t)n * it.stride + m);
-            v = load_value(c.in, c.in_type, e);
-            if (c.step) {
-                const float mo = c.momentum_out[e];
-                v = c.nesterov ? fmaf(c.beta, mo, v) : mo;
-            }
-            v = (float)((double)v * factor);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t r = slow + 16u * q, k = fast + e;
+            tile[t ? k : r][t ? r : k] = (float)((double)v[q][e] * factor);
         }
-        tile[tall(it) ? fast : slow][tall(it) ? slow : fast] = v;
-    }
     __syncthreads();
     // 2 x 4 fragments of each kind, two of each to a wave
     for (uint32_t f = wave; f < 16; f += 4) {
@@ -729,27 +749,45 @@ struct Plane {
     __device__ uint8_t* frag(uint32_t rb, uint32_t kb) const { return base + ((uint64_t)rb * per_row + kb) * kFragBytes; }
 };
 
-// blocks b = w PER + e of the nb x nb ones
+// blocks b = w PER + e of the nb x nb ones.  The three terms have sums of their own, so that products do not wait for each
+// other, and the fragments of two steps are on their way together.
 template <int PER>
 __device__ __forceinline__ void chain_product(float16v (&acc)[PER], const Plane& l, const Plane& r, uint32_t nb, uint32_t steps, uint32_t wave, uint32_t lane)
 {
+    float16v hl[PER], lh[PER];
 #pragma unroll
     for (int e = 0; e < PER; ++e)
 #pragma unroll
-        for (int k = 0; k < 16; ++k) acc[e][k] = 0.f;
+        for (int k = 0; k < 16; ++k) acc[e][k] = hl[e][k] = lh[e][k] = 0.f;
     if (wave * PER >= nb * nb) return;
-    for (uint32_t k = 0; k < steps; ++k) {
+    for (uint32_t k = 0; k < steps; k += 2) {
+        half8 left[2][PER][2], right[2][PER][2];
 #pragma unroll
-        for (int e = 0; e < PER; ++e) {
-            const uint32_t b = min(wave * PER + e, nb * nb - 1), i = b / nb, j = b - i * nb;
-            const uint8_t *pl = l.frag(i, k) + lane * 16u, *pr = r.frag(j, k) + lane * 16u;
-            const half8 lh = *reinterpret_cast<const half8*>(pl), ll = *reinterpret_cast<const half8*>(pl + 1024);
-            const half8 rh = *reinterpret_cast<const half8*>(pr), rl = *reinterpret_cast<const half8*>(pr + 1024);
-            acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lh, rl, acc[e], 0, 0, 0);
-            acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ll, rh, acc[e], 0, 0, 0);
-            acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lh, rh, acc[e], 0, 0, 0);
+        for (uint32_t u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < PER; ++e) {
+                const uint32_t b = min(wave * PER + e, nb * nb - 1), i = b / nb, j = b - i * nb, kk = min(k + u, steps - 1);
+                const uint8_t *pl = l.frag(i, kk) + lane * 16u, *pr = r.frag(j, kk) + lane * 16u;
+                left[u][e][0] = *reinterpret_cast<const half8*>(pl);
+                left[u][e][1] = *reinterpret_cast<const half8*>(pl + 1024);
+                right[u][e][0] = *reinterpret_cast<const half8*>(pr);
+                right[u][e][1] = *reinterpret_cast<const half8*>(pr + 1024);
+            }
+#pragma unroll
+        for (uint32_t u = 0; u < 2; ++u) {
+            if (k + u >= steps) break;
+#pragma unroll
+            for (int e = 0; e < PER; ++e) {
+                hl[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(left[u][e][0], right[u][e][1], hl[e], 0, 0, 0);
+                lh[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(left[u][e][1], right[u][e][0], lh[e], 0, 0, 0);
+                acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(left[u][e][0], right[u][e][0], acc[e], 0, 0, 0);
+            }
         }
     }
+#pragma unroll
+    for (int e = 0; e < PER; ++e)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) acc[e][k] += hl[e][k] + lh[e][k];
 }
 // four values of one column to a matrix's fragments (of its transpose, which it equals)
 __device__ __forceinline__ void chain_write(const Plane& to, uint32_t i, uint32_t j, uint32_t q, const float* v, uint32_t lane)
@@ -844,7 +882,7 @@ __device__ __forceinline__ void chain_gram(const ChainArgs& g, const Item& it, u
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
     const uint32_t steps = (it.m + 15u) / 16u;
     const Plane x{g.c.ws + by_rows(it, g.phase), it.mf};
-    constexpr uint32_t kAhead = 4;  // steps whose fragments are on their way together
+    constexpr uint32_t kAhead = 6;  // steps whose fragments are on their way together
     for (uint32_t k = wave; k < steps; k += kChainWaves * kAhead) {
         half8 h[kAhead][NB], l[kAhead][NB];
 #pragma unroll
