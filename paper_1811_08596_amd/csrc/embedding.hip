@@ -70,7 +70,10 @@ __device__ __forceinline__ void fill_chunk(const FillArgs& f, uint64_t i)
         for (uint64_t j = 0; c + j < f.row_values; ++j) out[j] = base ? base[j] : (U)0;
     }
 }
-// chunks of the launch's share that begins at `first`, by `count` workgroups
+// Chunks [first, end), by `count` workgroups: as a rule one a thread, in the order the workgroups begin in, so that all of them
+// together write one stretch at a time, which the memory takes at 6.8 TB/s (400 to 1000 MB; half a million threads that
+// go round, 4.5 to 4.9).
+constexpr uint32_t kMostFillers = 1u << 21;
 __device__ __forceinline__ void fill(const FillArgs& f, uint64_t first, uint64_t end, uint32_t index, uint32_t count)
 {
     const uint64_t step = (uint64_t)count * blockDim.x;
@@ -306,7 +309,7 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortArgs s, int p
 }
 
 // nothing to sort
-__global__ void __launch_bounds__(kOneThreads) k_fill(FillArgs f) { fill(f, 0, f.chunks, blockIdx.x, gridDim.x); }
+__global__ void __launch_bounds__(256) k_fill(FillArgs f) { fill(f, 0, f.chunks, blockIdx.x, gridDim.x); }
 
 // ---- sums over the sorted places ----
 struct SumArgs {
@@ -355,7 +358,7 @@ __device__ __forceinline__ void write_partial(const SumArgs& a, uint32_t stretch
 
 // A wave has a stretch of the sorted places and 64 V columns; kAhead rows are on their way together.
 constexpr uint32_t kAhead = 8;
-template <typename TI, typename TO, int V>
+template <typename TI, typename TO, int V, bool ADD>
 __global__ void __launch_bounds__(256) k_sum_stretches(SumArgs a, uint32_t slabs)
 {
     const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4u + (threadIdx.x >> 6)), lane = threadIdx.x & 63u;
@@ -376,7 +379,7 @@ __global__ void __launch_bounds__(256) k_sum_stretches(SumArgs a, uint32_t slabs
         if (at == first) head = first > 0 && a.sorted[first - 1].x == (uint32_t)__builtin_amdgcn_readfirstlane((int)own.x);
         for (uint32_t p = 0; p < here; p += kAhead) {
             Run<TI, V> x[kAhead];
-            Run<TO, V> y[kAhead];
+            Run<TO, V> y[ADD ? kAhead : 1];
             uint32_t row[kAhead + 1];
 #pragma unroll
             for (uint32_t u = 0; u <= kAhead; ++u)
@@ -388,8 +391,8 @@ __global__ void __launch_bounds__(256) k_sum_stretches(SumArgs a, uint32_t slabs
                 if (n == V) {
                     x[u] = load_run<TI, V>(r);
                     // what is in the table's row already, where a run ends
-                    if (a.add && p + u < here && row[u] != row[u + 1] && row[u] < a.rows)
-                        y[u] = load_run<TO, V>(static_cast<const TO*>(a.out) + (size_t)row[u] * a.out_stride + c);
+                    if (ADD && p + u < here && row[u] != row[u + 1] && row[u] < a.rows)
+                        y[ADD ? u : 0] = load_run<TO, V>(static_cast<const TO*>(a.out) + (size_t)row[u] * a.out_stride + c);
                 } else {
 #pragma unroll
                     for (uint32_t i = 0; i < V; ++i) x[u].v[i] = i < n ? r[i] : TI{};
@@ -405,7 +408,7 @@ __global__ void __launch_bounds__(256) k_sum_stretches(SumArgs a, uint32_t slabs
                 if (row[u] == row[u + 1] && !last) continue;
                 if (head) write_partial<V>(a, stretch, 0, c, n, acc);
                 else if (row[u] == row[u + 1]) write_partial<V>(a, stretch, 1, c, n, acc);
-                else write_row<TO, V>(a, row[u], c, n, acc, y[u]);
+                else write_row<TO, V>(a, row[u], c, n, acc, y[ADD ? u : 0]);
 #pragma unroll
                 for (int i = 0; i < V; ++i) acc[i] = 0.f;
                 head = false;
@@ -474,10 +477,13 @@ __global__ void __launch_bounds__(256) k_join_runs(SumArgs a)
 // ---- up to kFew places: no sorting, one launch ----
 // A workgroup per place and slab of 64 V columns compares its token with all others; if it is the first with that token, it sums
 // the rows of all of them, its waves eight rows at a time in turn.  Other workgroups fill the rows that no token has.
-constexpr uint32_t kFew = 1024, kFewRows = 16384;  // places; rows that one workgroup fills at most
+constexpr uint32_t kFew = 2048;           // places
+constexpr uint32_t kFewRows = 1u << 18;   // rows whose bits a workgroup holds
+constexpr uint64_t kFewBytes = 32 << 20;   // of a table that is filled beside the sums
+constexpr uint64_t kFewTokens = 1u << 23;  // tokens that the workgroups read in all: 64 MB
 struct FewArgs {
     EmbeddingArgs e;  // source: the rows' gradients, out: the table's
-    uint32_t slabs, fillers, per_filler, lanes;
+    uint32_t slabs, fillers, lanes;
 };
 template <typename TI, typename TO, int V>
 __global__ void __launch_bounds__(256) k_gradient_few(FewArgs f)
@@ -487,21 +493,21 @@ __global__ void __launch_bounds__(256) k_gradient_few(FewArgs f)
     const TO* base = static_cast<const TO*>(a.base);
     TO* out = static_cast<TO*>(a.out);
     if (blockIdx.x >= count * f.slabs) {
-        __shared__ uint32_t has[kFewRows / 32];
-        const uint64_t first = (uint64_t)(blockIdx.x - count * f.slabs) * f.per_filler, end = min((uint64_t)a.rows, first + f.per_filler);
-        for (uint32_t i = tid; i < (f.per_filler + 31u) / 32u; i += 256) has[i] = 0;
+        // rows that have a token, by bit; then rows in turn, `per` to a workgroup, so that all write one stretch at a time
+        extern __shared__ uint32_t has[];
+        const uint32_t index = blockIdx.x - count * f.slabs, li = tid & (f.lanes - 1u), per = 256u / f.lanes, rows = (uint32_t)a.rows;
+        for (uint32_t i = tid; i < (rows + 31u) / 32u; i += 256) has[i] = 0;
         __syncthreads();
         for (uint32_t t = tid; t < count; t += 256) {
-            const uint32_t row = token_row(a.tokens, a.token_bits, t, (uint32_t)a.rows);
-            if (row >= first && row < end) atomicOr(&has[(row - first) / 32u], 1u << ((row - first) & 31u));
+            const uint32_t row = token_row(a.tokens, a.token_bits, t, rows);
+            if (row < rows) atomicOr(&has[row / 32u], 1u << (row & 31u));
         }
         __syncthreads();
         constexpr uint32_t W = 16 / sizeof(TO);
-        const uint32_t li = tid & (f.lanes - 1u), per = 256u / f.lanes;
-        for (uint64_t row = first + tid / f.lanes; row < end; row += per) {
-            if (has[(row - first) / 32u] >> ((row - first) & 31u) & 1u) continue;
+        for (uint32_t row = index * per + tid / f.lanes; row < rows; row += f.fillers * per) {
+            if (has[row / 32u] >> (row & 31u) & 1u) continue;
             for (uint32_t c = li * W; c < a.width; c += f.lanes * W) {
-                const uint64_t at = row * a.out_stride + c;
+                const uint64_t at = (uint64_t)row * a.out_stride + c;
                 if (c + W <= a.width) {
                     Run<TO, W> x{};
                     if (base) x = load_run<TO, W>(base + at);
@@ -613,8 +619,6 @@ uint32_t lanes_for(uint32_t width, uint32_t v)
 // values a lane has of a row of type bytes: 16 bytes
 constexpr int values_of(size_t bytes) { return bytes == 4 ? 4 : 8; }
 
-constexpr uint32_t kFillThreads = 256 * 2048;  // that fill at once: what the card holds
-
 struct GradientPlan {
     uint32_t blocks, stretch, stretches;
     int passes;
@@ -627,7 +631,7 @@ GradientPlan gradient_plan(size_t rows, uint32_t width, size_t count)
     p.blocks = (uint32_t)((count + kSortBlock - 1) / kSortBlock);
     const size_t slabs = (width + 511u) / 512u;
     p.stretch = 16;
-    while (count * slabs / p.stretch > 4096) p.stretch *= 2;
+    while (count * slabs / p.stretch > 8192) p.stretch *= 2;
     p.stretches = (uint32_t)((count + p.stretch - 1) / p.stretch);
     size_t off = 0;
     p.a = off;       off = align256(off + count * 8);
@@ -674,24 +678,29 @@ hipError_t launch_embedding_gradient(const EmbeddingArgs& a, uint8_t* ws, hipStr
         f.per_row = (f.row_values * f.bytes + 15) / 16;
         f.chunks = f.per_row * (flat ? 1 : a.rows);
     }
-    auto fillers = [&](uint64_t chunks, uint32_t threads) { return (uint32_t)std::min<uint64_t>((chunks + threads - 1) / threads, kFillThreads / threads); };
+    auto fillers = [](uint64_t chunks, uint32_t threads) { return (uint32_t)std::min<uint64_t>((chunks + threads - 1) / threads, kMostFillers); };
     if (a.ntokens == 0) {
-        if (f.chunks) FFTSP_LAUNCH("embedding_fill", k_fill, dim3(fillers(f.chunks, kOneThreads)), dim3(kOneThreads), 0, s, f);
+        if (f.chunks) FFTSP_LAUNCH("embedding_fill", k_fill, dim3(fillers(f.chunks, 256)), dim3(256), 0, s, f);
         return hipGetLastError();
     }
-    if (a.ntokens <= kFew) {
+    const uint32_t in_values = values_of(type_bytes(a.source_type)), few_slabs = (a.width + 64u * in_values - 1u) / (64u * in_values);
+    if (a.ntokens <= kFew && a.ntokens * a.ntokens * few_slabs <= kFewTokens) {
+        // small tables are filled beside the sums, larger ones by a launch before, which writes at the memory's rate
+        const bool beside = a.rows <= kFewRows && f.chunks * 16 <= kFewBytes;
+        if (f.chunks && !beside) FFTSP_LAUNCH("embedding_fill", k_fill, dim3(fillers(f.chunks, 256)), dim3(256), 0, s, f);
         return with_type(a.source_type, [&](auto ti) {
             return with_type(a.out_type, [&](auto to) {
                 using TI = decltype(ti);
                 using TO = decltype(to);
                 constexpr int V = values_of(sizeof(TI));
-                FewArgs w{a, (a.width + 64u * V - 1u) / (64u * V), 0, 0, lanes_for(a.width, 16 / sizeof(TO))};
-                if (a.base != a.out) {
-                    // as many workgroups as fill the card, or more where their bitmaps would not hold the rows
-                    w.per_filler = (uint32_t)std::min<uint64_t>(kFewRows, (a.rows + 2047) / 2048);
-                    w.fillers = (uint32_t)((a.rows + w.per_filler - 1) / w.per_filler);
+                FewArgs w{a, few_slabs, 0, lanes_for(a.width, 16 / sizeof(TO))};
+                uint32_t lds = 0;
+                if (f.chunks && beside) {
+                    const uint64_t per = 256u / w.lanes;
+                    w.fillers = (uint32_t)std::min<uint64_t>((a.rows + per - 1) / per, 1024);
+                    lds = (uint32_t)(a.rows + 31) / 32 * 4;
                 }
-                FFTSP_LAUNCH("embedding_few", (k_gradient_few<TI, TO, V>), dim3((uint32_t)a.ntokens * w.slabs + w.fillers), dim3(256), 0, s, w);
+                FFTSP_LAUNCH("embedding_few", (k_gradient_few<TI, TO, V>), dim3((uint32_t)a.ntokens * few_slabs + w.fillers), dim3(256), lds, s, w);
                 return hipGetLastError();
             });
         });
@@ -703,7 +712,7 @@ hipError_t launch_embedding_gradient(const EmbeddingArgs& a, uint8_t* ws, hipStr
     if (one) {
         FFTSP_LAUNCH("embedding_sort_one", k_sort_one, dim3(1 + fillers(f.chunks, kOneThreads)), dim3(kOneThreads), 0, s, so);
     } else {
-        const dim3 grid(p.blocks + fillers(f.chunks / (p.passes + 1) + 1, kSortThreads) * (f.chunks ? 1 : 0));
+        const dim3 grid(p.blocks + fillers((f.chunks + p.passes) / (p.passes + 1), kSortThreads));
         FFTSP_LAUNCH("embedding_sort_count", k_sort_count, grid, dim3(kSortThreads), 0, s, so);
         for (int i = 0; i < p.passes; ++i) FFTSP_LAUNCH("embedding_sort", k_sort_scatter, grid, dim3(kSortThreads), 0, s, so, i);
     }
@@ -730,7 +739,9 @@ hipError_t launch_embedding_gradient(const EmbeddingArgs& a, uint8_t* ws, hipStr
             constexpr int V = values_of(sizeof(TI));
             const uint32_t slabs = (a.width + 64u * V - 1u) / (64u * V);
             const uint64_t waves = (uint64_t)p.stretches * slabs;
-            FFTSP_LAUNCH("embedding_sum", (k_sum_stretches<TI, TO, V>), dim3((uint32_t)((waves + 3) / 4)), dim3(256), 0, s, m, slabs);
+            const dim3 grid((uint32_t)((waves + 3) / 4));
+            if (m.add) FFTSP_LAUNCH("embedding_sum", (k_sum_stretches<TI, TO, V, true>), grid, dim3(256), 0, s, m, slabs);
+            else FFTSP_LAUNCH("embedding_sum", (k_sum_stretches<TI, TO, V, false>), grid, dim3(256), 0, s, m, slabs);
             if (p.stretches > 1) FFTSP_LAUNCH("embedding_join", (k_join_runs<TI, TO, V>), dim3(p.stretches, slabs), dim3(256), 0, s, m);
             return hipGetLastError();
         });
