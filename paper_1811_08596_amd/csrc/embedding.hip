@@ -616,8 +616,8 @@ uint32_t lanes_for(uint32_t width, uint32_t v)
     while (lanes < 256 && lanes * v < width) lanes <<= 1;
     return lanes;
 }
-// values a lane has of a row of type bytes: 16 bytes
-constexpr int values_of(size_t bytes) { return bytes == 4 ? 4 : 8; }
+// values a lane has of a row: 16 bytes of the wider of the two types, so that a wave's accesses to either are whole lines
+constexpr int values_of(size_t in_bytes, size_t out_bytes) { return in_bytes == 4 || out_bytes == 4 ? 4 : 8; }
 
 struct GradientPlan {
     uint32_t blocks, stretch, stretches;
@@ -629,7 +629,7 @@ GradientPlan gradient_plan(size_t rows, uint32_t width, size_t count)
     GradientPlan p{};
     p.passes = sort_passes(rows);
     p.blocks = (uint32_t)((count + kSortBlock - 1) / kSortBlock);
-    const size_t slabs = (width + 511u) / 512u;
+    const size_t slabs = (width + 255u) / 256u;
     p.stretch = 16;
     while (count * slabs / p.stretch > 8192) p.stretch *= 2;
     p.stretches = (uint32_t)((count + p.stretch - 1) / p.stretch);
@@ -683,7 +683,7 @@ hipError_t launch_embedding_gradient(const EmbeddingArgs& a, uint8_t* ws, hipStr
         if (f.chunks) FFTSP_LAUNCH("embedding_fill", k_fill, dim3(fillers(f.chunks, 256)), dim3(256), 0, s, f);
         return hipGetLastError();
     }
-    const uint32_t in_values = values_of(type_bytes(a.source_type)), few_slabs = (a.width + 64u * in_values - 1u) / (64u * in_values);
+    const uint32_t in_values = values_of(type_bytes(a.source_type), type_bytes(a.out_type)), few_slabs = (a.width + 64u * in_values - 1u) / (64u * in_values);
     if (a.ntokens <= kFew && a.ntokens * a.ntokens * few_slabs <= kFewTokens) {
         // small tables are filled beside the sums, larger ones by a launch before, which writes at the memory's rate
         const bool beside = a.rows <= kFewRows && f.chunks * 16 <= kFewBytes;
@@ -692,7 +692,7 @@ hipError_t launch_embedding_gradient(const EmbeddingArgs& a, uint8_t* ws, hipStr
             return with_type(a.out_type, [&](auto to) {
                 using TI = decltype(ti);
                 using TO = decltype(to);
-                constexpr int V = values_of(sizeof(TI));
+                constexpr int V = values_of(sizeof(TI), sizeof(TO));
                 FewArgs w{a, few_slabs, 0, lanes_for(a.width, 16 / sizeof(TO))};
                 uint32_t lds = 0;
                 if (f.chunks && beside) {
@@ -736,7 +736,7 @@ hipError_t launch_embedding_gradient(const EmbeddingArgs& a, uint8_t* ws, hipStr
         return with_type(a.out_type, [&](auto to) {
             using TI = decltype(ti);
             using TO = decltype(to);
-            constexpr int V = values_of(sizeof(TI));
+            constexpr int V = values_of(sizeof(TI), sizeof(TO));
             const uint32_t slabs = (a.width + 64u * V - 1u) / (64u * V);
             const uint64_t waves = (uint64_t)p.stretches * slabs;
             const dim3 grid((uint32_t)((waves + 3) / 4));
