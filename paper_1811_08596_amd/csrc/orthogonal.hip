@@ -7,8 +7,8 @@
 // That is n^2 m for A and 2 n^2 m for Q X once a phase instead of once a step, and four symmetric n x n products (n^3
 // each: only tiles on and under the diagonal are computed, and written twice) a step instead of one.  A has an absolute error
 // of 2^-24 of its largest eigenvalue, which the small eigenvalues' growth by a^2 a step turns into a relative one: 1e-6 after
-// two steps, 3.4445^4 2^-24 = 1e-5 after three, 1e-3 after five.  So a phase has up to two steps where the result is stored in
-// 32 bits, up to three where it is rounded to 16.
+// two steps, 3.4445^4 2^-24 = 1e-5 after three, 1e-3 after five.  So a phase has one step or two where the result is stored in
+// 32 bits (plan_of), up to three where it is rounded to 16.  Lists of small matrices take none of this: k_whole.
 //
 // Products run on binary16 matrix instructions whose inputs carry a binary32 number in two planes: 2^e v = hi + lo, each
 // rounded to nearest (v is then 2^-24 v off, or 2^-(25 + e) where v is small), and x y = hi hi + hi lo + lo hi summed in
@@ -25,6 +25,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <type_traits>
 #include <vector>
 
 namespace fftsp {
@@ -44,7 +45,7 @@ enum Square { kA, kP, kT, kQ0, kQ1, kSquares };
 // Launches of products by what they contract: X X^T, one or two products of n x n by n x n, and n x n by X.
 enum Class { kGrams, kSingles, kPairs, kWides, kClasses };
 // What the workgroups of a launch do: how many the matrices before each have, by kind of launch.
-enum Kind { kNorm, kConvert, kChain, kProducts, kKinds = kProducts + kClasses };
+enum Kind { kNorm, kConvert, kProducts, kKinds = kProducts + kClasses };
 
 // A matrix as the kernels see it.  Offsets are bytes from the workspace's start.
 struct Item {
@@ -55,8 +56,6 @@ struct Item {
     uint32_t nf, mf;            // fragments along n and along m that there is room for
     uint32_t parts;             // workgroups that sum its squares
     float gain;
-    uint32_t chain;             // 1: one workgroup does its phase, 2: X X^T, too
-    uint32_t pad;
 };
 __device__ __forceinline__ bool tall(const Item& it) { return it.rows > it.cols; }
 __device__ __forceinline__ uint64_t by_rows(const Item& it, int phase) { return phase & 1 ? it.x[1] : it.x[0]; }
@@ -728,242 +727,385 @@ __global__ void __launch_bounds__(S::kThreads, 2) k_product(ProductArgs g)
     finish<S, WHAT>(g, it, product, acc, lds, ti, tj, wave, lane);
 }
 
-// ---- a whole phase of a small matrix (n <= 128): one workgroup, A, P and (n <= 96) Q in LDS ----
-struct ChainStep {
-    float ca, cb, poly, t, q, a;  // as in ProductArgs, for P, P A, P Q and A's
+// ---- small matrices (n <= 64, m <= 768): one workgroup each, everything in one launch, X in registers ----
+// A launch that depends on the one before takes 4 us whatever it does, and a step has three of them.  Wave w has the columns
+// 32 (w + 8 b) .. + 31 of X as fragments whose rows are those columns (three such blocks are 96 registers of its 256; a fourth
+// spills).  The accumulators of P X are X's next fragments, and their products by the identity, which are exact, those of X's
+// rows, which go into X X^T at once.  Only X X^T, summed over the waves, A and P are in LDS.  A lane's accumulators hold rows
+// 8 (e / 4) + 4 (l / 32) + e % 4 of a block, so that is the order of the contracted index in all fragments here.
+// Five steps, 32 bits: 64 x 64 takes 25 us, 64 x 768 60 and as launches of products (64 x 769) 93; 1024 of these 327 and 1774,
+// 2048 of 64 x 64 261 and (65 x 65) 1436.  A step of 64 x 576 takes 6.6 us: 50 matrix instructions a block of columns are 3.5
+// on a SIMD that has five blocks, and the sum over the waves, A and P, which wait for each other, the rest.
+struct WholeStep {
+    float gram, ca, cb, poly, apply;  // scales of the sums, and what P has besides, as in ProductArgs
 };
-struct ChainArgs {
+struct WholeArgs {
     Common c;
-    ChainStep step[kPhaseMost];
-    int steps, phase, q;  // q: where the apply looks for Q
-    float gram;
+    WholeStep step[kMostSteps];
+    int steps;
+    const MatrixSpan* items;
 };
-constexpr int kChainThreads = 512, kChainWaves = 8;
-constexpr uint32_t kChainMost = 128, kChainGram = 64, kChainGramSteps = 512;  // n; n and steps of X X^T that the same workgroup does
-constexpr uint32_t kChainLds = 128 * 1024;
-
-// fragments of a matrix: row block rb, step kb
-struct Plane {
-    uint8_t* base;
-    uint32_t per_row;
-    __device__ uint8_t* frag(uint32_t rb, uint32_t kb) const { return base + ((uint64_t)rb * per_row + kb) * kFragBytes; }
+constexpr uint32_t kWholeHeight = 64, kWholeWidth = 768;  // n and m at most
+constexpr int kWholeThreads = 512, kWholeWaves = 8, kWholeBlocks = kWholeWidth / 32 / kWholeWaves;
+constexpr uint64_t kWholeExtent = 1 << 29;                 // elements from a matrix's first to its last: byte offsets in 32 bits
+constexpr int kWholeItems = 64;  // in a launch's arguments
+// in LDS: sums of X X^T by wave, block under the diagonal, quarter of it and lane; A; P
+template <int NB>
+struct WholeLds {
+    static constexpr int kUnits = NB * (NB + 1) / 2 * 4;
+    static constexpr uint32_t kPlane = NB * 2 * NB * kFragBytes, kA = kWholeWaves * kUnits * 1024, kP = kA + kPlane, kBytes = kP + kPlane;
 };
-
-// blocks b = w PER + e of the nb x nb ones.  The three terms have sums of their own, so that products do not wait for each
-// other, and the fragments of two steps are on their way together.
-template <int PER>
-__device__ __forceinline__ void chain_product(float16v (&acc)[PER], const Plane& l, const Plane& r, uint32_t nb, uint32_t steps, uint32_t wave, uint32_t lane)
+struct WholeTable {
+    MatrixSpan item[kWholeItems];
+    uint32_t first, count;
+};
+__global__ void k_whole_items(WholeTable t, MatrixSpan* items)
 {
-    float16v hl[PER], lh[PER];
-#pragma unroll
-    for (int e = 0; e < PER; ++e)
-#pragma unroll
-        for (int k = 0; k < 16; ++k) acc[e][k] = hl[e][k] = lh[e][k] = 0.f;
-    if (wave * PER >= nb * nb) return;
-    for (uint32_t k = 0; k < steps; k += 2) {
-        half8 left[2][PER][2], right[2][PER][2];
-#pragma unroll
-        for (uint32_t u = 0; u < 2; ++u)
-#pragma unroll
-            for (int e = 0; e < PER; ++e) {
-                const uint32_t b = min(wave * PER + e, nb * nb - 1), i = b / nb, j = b - i * nb, kk = min(k + u, steps - 1);
-                const uint8_t *pl = l.frag(i, kk) + lane * 16u, *pr = r.frag(j, kk) + lane * 16u;
-                left[u][e][0] = *reinterpret_cast<const half8*>(pl);
-                left[u][e][1] = *reinterpret_cast<const half8*>(pl + 1024);
-                right[u][e][0] = *reinterpret_cast<const half8*>(pr);
-                right[u][e][1] = *reinterpret_cast<const half8*>(pr + 1024);
-            }
-#pragma unroll
-        for (uint32_t u = 0; u < 2; ++u) {
-            if (k + u >= steps) break;
-#pragma unroll
-            for (int e = 0; e < PER; ++e) {
-                hl[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(left[u][e][0], right[u][e][1], hl[e], 0, 0, 0);
-                lh[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(left[u][e][1], right[u][e][0], lh[e], 0, 0, 0);
-                acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_f16(left[u][e][0], right[u][e][0], acc[e], 0, 0, 0);
-            }
-        }
-    }
-#pragma unroll
-    for (int e = 0; e < PER; ++e)
-#pragma unroll
-        for (int k = 0; k < 16; ++k) acc[e][k] += hl[e][k] + lh[e][k];
+    if (threadIdx.x < t.count) items[t.first + threadIdx.x] = t.item[threadIdx.x];
 }
-// four values of one column to a matrix's fragments (of its transpose, which it equals)
-__device__ __forceinline__ void chain_write(const Plane& to, uint32_t i, uint32_t j, uint32_t q, const float* v, uint32_t lane)
+
+__device__ __forceinline__ void split8(const float* v, half8* hi, half8* lo)
 {
-    half4 hi, lo;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < 8; ++e) {
         _Float16 h, l;
         split(v[e], &h, &l);
-        hi[e] = h;
-        lo[e] = l;
+        (*hi)[e] = h;
+        (*lo)[e] = l;
     }
-    uint8_t* dst = to.frag(j, i * 2u + q / 2u) + ((lane & 31u) + 32u * (q & 1u)) * 16u + (lane >> 5) * 8u;
-    *reinterpret_cast<half4*>(dst) = hi;
-    *reinterpret_cast<half4*>(dst + 1024) = lo;
 }
-template <int PER>
-__device__ __forceinline__ void chain_store(const Plane& to, const float16v (&acc)[PER], float scale, uint32_t nb, uint32_t wave, uint32_t lane)
+__device__ __forceinline__ float16v zeros()
 {
+    float16v z;
 #pragma unroll
-    for (int e = 0; e < PER; ++e) {
-        const uint32_t b = wave * PER + e;
-        if (b >= nb * nb) continue;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            float v[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = acc[e][4 * q + k] * scale;
-            chain_write(to, b / nb, b % nb, q, v, lane);
-        }
-    }
+    for (int e = 0; e < 16; ++e) z[e] = 0.f;
+    return z;
+}
+__device__ __forceinline__ float16v product3(half8 lh, half8 ll, half8 rh, half8 rl, float16v acc)
+{
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(lh, rl, acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ll, rh, acc, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(lh, rh, acc, 0, 0, 0);
 }
 
-template <int PER>
-__device__ __forceinline__ void chain_steps(const ChainArgs& g, const Item& it, uint8_t* lds, uint32_t nb, uint32_t wave, uint32_t lane)
+// U's values of the wave's columns, as fragments whose rows are the caller's columns: of X by columns where it lies as the
+// caller's array does, of X by rows where it is the transpose.  The momentum is written down.  Returns the squares' sum.
+// Every access is within the matrix: the places outside read its last row or column, and count as zero.
+template <int NB, typename T, bool STEP>
+__device__ __forceinline__ double whole_load(const Common& c, const MatrixSpan& it, uint32_t blocks, uint32_t wave, uint32_t lane,
+                                             float (&v)[kWholeBlocks][2 * NB][8])
 {
-    const uint32_t steps = (it.n + 15u) / 16u, bytes = nb * nb * 2u * kFragBytes;
-    const Plane a{lds, 2 * nb}, p{lds + bytes, 2 * nb}, out{g.c.ws + it.square + g.q * it.square_bytes, it.nf};
-    const Plane q = nb < 4 ? Plane{lds + 2 * bytes, 2 * nb} : out;
-    for (int s = 0; s < g.steps; ++s) {
-        const ChainStep& st = g.step[s];
-        const bool again = s + 1 < g.steps;
-        {
-            float16v acc[PER];
-            chain_product<PER>(acc, a, a, nb, steps, wave, lane);
+    const bool t = it.rows > it.cols;
+    const T* in_values = static_cast<const T*>(c.in) + it.offset;
+    const float* momentum = c.momentum + it.offset;
+    float* momentum_out = c.momentum_out + it.offset;
+    const uint32_t stride = (uint32_t)it.stride;
+    auto place = [&](int b, int k, int e, uint32_t* at) {
+        const uint32_t bj = b * kWholeWaves + wave, o = 8u * (e / 4) + 4u * (lane >> 5) + e % 4;
+        const uint32_t row = t ? bj * 32u + (k & 1) * 16u + o : k * 16u + o, col = (t ? k >> 1 : bj) * 32u + (lane & 31u);
+        *at = min(row, it.rows - 1) * stride + min(col, it.cols - 1);
+        return row < it.rows && col < it.cols;
+    };
+    float mo[kWholeBlocks][2 * NB][8];
 #pragma unroll
-            for (int e = 0; e < PER; ++e) {
-                const uint32_t b = wave * PER + e, i = b / nb, j = b % nb;
-                if (b >= nb * nb) continue;
+    for (int b = 0; b < kWholeBlocks; ++b) {
+        const bool some = b * kWholeWaves + wave < blocks;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint8_t* src = a.frag(j, i * 2u + k / 2u) + ((lane & 31u) + 32u * (k & 1u)) * 16u + (lane >> 5) * 8u;
-                    const half4 ah = *reinterpret_cast<const half4*>(src), al = *reinterpret_cast<const half4*>(src + 1024);
-                    float v[4];
+        for (int k = 0; k < 2 * NB; ++k)
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        v[t] = fmaf(st.cb, (float)ah[t] + (float)al[t], acc[e][4 * k + t] * st.poly);
-                        if (i == j && (lane & 31u) == 8u * k + 4u * (lane >> 5) + t) v[t] += st.ca;
-                    }
-                    if (again || s) chain_write(p, i, j, k, v, lane);
-                    if (s == 0) chain_write(again ? q : out, i, j, k, v, lane);
+            for (int e = 0; e < 8; ++e) {
+                uint32_t at;
+                place(b, k, e, &at);
+                v[b][k][e] = mo[b][k][e] = 0.f;
+                if (some) {
+                    v[b][k][e] = to_float(in_values[at]);
+                    if (STEP) mo[b][k][e] = momentum[at];
                 }
             }
-        }
-        __syncthreads();
-        float16v t[PER], w[PER];
-        if (again) chain_product<PER>(t, p, a, nb, steps, wave, lane);
-        if (s) chain_product<PER>(w, p, q, nb, steps, wave, lane);
-        __syncthreads();
-        if (again) chain_store<PER>(a, t, st.t, nb, wave, lane);  // T in A's place
-        if (s) chain_store<PER>(again ? q : out, w, st.q, nb, wave, lane);
-        __syncthreads();
-        if (again) {
-            chain_product<PER>(t, a, p, nb, steps, wave, lane);
-            __syncthreads();
-            chain_store<PER>(a, t, st.a, nb, wave, lane);
-            __syncthreads();
-        }
     }
+    double s = 0.0;
+#pragma unroll
+    for (int b = 0; b < kWholeBlocks; ++b) {
+        if (b * kWholeWaves + wave >= blocks) break;
+#pragma unroll
+        for (int k = 0; k < 2 * NB; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                uint32_t at;
+                const bool in = place(b, k, e, &at);
+                float u = v[b][k][e];
+                if (STEP) {
+                    const float m = fmaf(c.beta, mo[b][k][e], u);
+                    if (in) momentum_out[at] = m;
+                    u = c.nesterov ? fmaf(c.beta, m, u) : m;
+                }
+                u = in ? u : 0.f;
+                s += (double)u * (double)u;
+                v[b][k][e] = u;
+            }
+    }
+    return s;
 }
 
-// A = X X^T of n <= 32 NB: every wave has an eighth of the steps
+// A = scale X X^T from the waves' parts: a unit is a quarter of a block under the diagonal, which is A's both ways round
 template <int NB>
-__device__ __forceinline__ void chain_gram(const ChainArgs& g, const Item& it, uint8_t* lds, uint32_t wave, uint32_t lane)
+__device__ __forceinline__ void whole_sum(uint8_t* lds, float scale, uint32_t parts, uint32_t wave, uint32_t lane)
 {
-    float16v acc[NB][NB];
+    using L = WholeLds<NB>;
+    const float4* sums = reinterpret_cast<const float4*>(lds);
+    uint8_t* a = lds + L::kA;
+    for (uint32_t unit = wave; unit < L::kUnits; unit += kWholeWaves) {
+        float v[4] = {};
+        for (uint32_t w = 0; w < parts; ++w) {
+            const float4 f = sums[(w * L::kUnits + unit) * 64 + lane];
+            v[0] += f.x;
+            v[1] += f.y;
+            v[2] += f.z;
+            v[3] += f.w;
+        }
+        const uint32_t b = unit / 4, q = unit % 4, i = b ? 1 : 0, j = b == 2 ? 1 : 0;  // blocks (0, 0), (1, 0), (1, 1)
+        const uint32_t col = lane & 31u, half = lane >> 5;
+        half4 hi, lo;
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
+        for (int e = 0; e < 4; ++e) {
+            _Float16 h, l;
+            split(v[e] * scale, &h, &l);
+            hi[e] = h;
+            lo[e] = l;
+        }
+        uint8_t* dst = a + (j * 2 * NB + i * 2 + q / 2) * kFragBytes + lane * 16u + (q & 1u) * 8u;
+        *reinterpret_cast<half4*>(dst) = hi;
+        *reinterpret_cast<half4*>(dst + 1024) = lo;
+        if (i == j) continue;
+        uint8_t* to = a + (i * 2 * NB + j * 2 + col / 16) * kFragBytes + (8u * q + 4u * half + 32u * (col >> 2 & 1u)) * 16u + ((col >> 3 & 1u) * 4u + (col & 3u)) * 2u;
 #pragma unroll
-        for (int j = 0; j < NB; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-    const uint32_t steps = (it.m + 15u) / 16u;
-    const Plane x{g.c.ws + by_rows(it, g.phase), it.mf};
-    constexpr uint32_t kAhead = 6;  // steps whose fragments are on their way together
-    for (uint32_t k = wave; k < steps; k += kChainWaves * kAhead) {
-        half8 h[kAhead][NB], l[kAhead][NB];
-#pragma unroll
-        for (uint32_t u = 0; u < kAhead; ++u)
-#pragma unroll
-            for (int i = 0; i < NB; ++i) {
-                const uint8_t* src = x.frag(i, min(k + u * kChainWaves, steps - 1)) + lane * 16u;
-                h[u][i] = *reinterpret_cast<const half8*>(src);
-                l[u][i] = *reinterpret_cast<const half8*>(src + 1024);
-            }
-#pragma unroll
-        for (uint32_t u = 0; u < kAhead; ++u) {
-            if (k + u * kChainWaves >= steps) break;
-#pragma unroll
-            for (int i = 0; i < NB; ++i)
-#pragma unroll
-                for (int j = 0; j < NB; ++j) {
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(h[u][i], l[u][j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[u][i], h[u][j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(h[u][i], h[u][j], acc[i][j], 0, 0, 0);
-                }
+        for (int e = 0; e < 4; ++e) {
+            *reinterpret_cast<_Float16*>(to + e * 16) = hi[e];
+            *reinterpret_cast<_Float16*>(to + e * 16 + 1024) = lo[e];
         }
     }
-    float4* sums = reinterpret_cast<float4*>(lds);  // [wave][block][4][lane]
+}
+
+// P = a I + b A + c A A: a wave has a block; the three terms have sums of their own, so that products do not wait for each other
+template <int NB>
+__device__ __forceinline__ void whole_poly(uint8_t* lds, const WholeStep& st, uint32_t steps, uint32_t wave, uint32_t lane)
+{
+    using L = WholeLds<NB>;
+    if (wave >= NB * NB) return;
+    const uint32_t i = wave / NB, j = wave % NB;
+    const uint8_t* a = lds + L::kA + lane * 16u;
+    float16v sum[3] = {zeros(), zeros(), zeros()};
+#pragma unroll
+    for (uint32_t k = 0; k < 2 * NB; ++k) {
+        if (k >= steps) break;
+        const uint8_t *pl = a + (i * 2 * NB + k) * kFragBytes, *pr = a + (j * 2 * NB + k) * kFragBytes;
+        const half8 lh = *reinterpret_cast<const half8*>(pl), ll = *reinterpret_cast<const half8*>(pl + 1024);
+        const half8 rh = *reinterpret_cast<const half8*>(pr), rl = *reinterpret_cast<const half8*>(pr + 1024);
+        sum[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lh, rl, sum[0], 0, 0, 0);
+        sum[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ll, rh, sum[1], 0, 0, 0);
+        sum[2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lh, rh, sum[2], 0, 0, 0);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const uint32_t at = (j * 2 * NB + i * 2 + k) * kFragBytes;
+        const half8 ah = *reinterpret_cast<const half8*>(a + at), al = *reinterpret_cast<const half8*>(a + at + 1024);
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float s = sum[2][8 * k + e] + (sum[0][8 * k + e] + sum[1][8 * k + e]);
+            v[e] = fmaf(st.cb, (float)ah[e] + (float)al[e], s * st.poly);
+            if (i == j && (lane & 31u) == 16u * k + 8u * (e / 4) + 4u * (lane >> 5) + e % 4) v[e] += st.ca;
+        }
+        half8 hi, lo;
+        split8(v, &hi, &lo);
+        uint8_t* dst = lds + L::kP + at + lane * 16u;
+        *reinterpret_cast<half8*>(dst) = hi;
+        *reinterpret_cast<half8*>(dst + 1024) = lo;
+    }
+}
+
+// P times a block of columns, or the block's transpose times P
+template <int NB, bool TURNED>
+__device__ __forceinline__ void whole_times(const uint8_t* p, const half8* xh, const half8* xl, uint32_t steps, float16v (&acc)[NB])
+{
+#pragma unroll
+    for (int i = 0; i < NB; ++i) acc[i] = zeros();
+#pragma unroll
+    for (uint32_t k = 0; k < 2 * NB; ++k) {
+        if (k >= steps) break;
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            const uint8_t* src = p + (i * 2 * NB + k) * kFragBytes;
+            const half8 h = *reinterpret_cast<const half8*>(src), l = *reinterpret_cast<const half8*>(src + 1024);
+            acc[i] = TURNED ? product3(xh[k], xl[k], h, l, acc[i]) : product3(h, l, xh[k], xl[k], acc[i]);
+        }
+    }
+}
+// Fragments of a block's transpose: products by the identity, which are exact
+template <int NB>
+__device__ __forceinline__ void whole_turn(const half8 (&one)[2], const half8* from, half8* to)
+{
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+        float16v acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(from[2 * i], one[0], zeros(), 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(from[2 * i + 1], one[1], acc, 0, 0, 0);
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) to[2 * i + k][e] = (_Float16)acc[8 * k + e];
+    }
+}
+template <int NB>
+__device__ __forceinline__ void whole_split(const float16v (&acc)[NB], float scale, half8* hi, half8* lo)
+{
 #pragma unroll
     for (int i = 0; i < NB; ++i)
 #pragma unroll
-        for (int j = 0; j < NB; ++j)
+        for (int k = 0; k < 2; ++k) {
+            float v[8];
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                sums[((wave * (NB * NB) + i * NB + j) * 4 + q) * 64 + lane] =
-                    make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-    __syncthreads();
-    constexpr int kUnits = NB * NB * 4, kEach = (kUnits + kChainWaves - 1) / kChainWaves;
-    float v[kEach][4];
-#pragma unroll
-    for (int u = 0; u < kEach; ++u) {
-        const uint32_t unit = wave * kEach + u;
-        v[u][0] = v[u][1] = v[u][2] = v[u][3] = 0.f;
-        if (unit < kUnits)
-            for (int w = 0; w < kChainWaves; ++w) {
-                const float4 f = sums[(w * kUnits + unit) * 64 + lane];
-                v[u][0] += f.x;
-                v[u][1] += f.y;
-                v[u][2] += f.z;
-                v[u][3] += f.w;
-            }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int u = 0; u < kEach; ++u) {
-        const uint32_t unit = wave * kEach + u, b = unit / 4;
-        if (unit >= kUnits) continue;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[u][e] *= g.gram;
-        chain_write(Plane{lds, 2 * NB}, b / NB, b % NB, unit % 4, v[u], lane);
-    }
-    __syncthreads();
+            for (int e = 0; e < 8; ++e) v[e] = acc[i][8 * k + e] * scale;
+            split8(v, hi + 2 * i + k, lo + 2 * i + k);
+        }
 }
 
-__global__ void __launch_bounds__(kChainThreads, 2) k_chain(ChainArgs g)
+// a block of the result: accumulators' columns are the caller's
+template <int NB, typename T>
+__device__ __forceinline__ void whole_store(const Common& c, const MatrixSpan& it, const float16v (&acc)[NB], float scale, uint32_t bj, uint32_t lane)
+{
+    const bool t = it.rows > it.cols;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+        const uint32_t row = (t ? bj : i) * 32u + 4u * (lane >> 5), col = (t ? i : bj) * 32u + (lane & 31u);
+        float w[16];
+        if (c.step)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const uint32_t r = row + 8u * (e / 4) + e % 4;
+                w[e] = r < it.rows && col < it.cols ? to_float(static_cast<const T*>(c.weights)[it.offset + (uint64_t)r * it.stride + col]) : 0.f;
+            }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const uint32_t r = row + 8u * (e / 4) + e % 4;
+            float v = acc[i][e] * scale;
+            if (c.step) v = fmaf(-c.lr, v, c.decay * w[e]);
+            if (r < it.rows && col < it.cols) static_cast<T*>(c.out)[it.offset + (uint64_t)r * it.stride + col] = from_float<T>(v);
+        }
+    }
+}
+
+template <int NB>
+__device__ __forceinline__ void whole(const WholeArgs& w, const MatrixSpan& it, uint8_t* lds, uint32_t wave, uint32_t lane)
+{
+    using L = WholeLds<NB>;
+    const Common& c = w.c;
+    const uint32_t steps = (min(it.rows, it.cols) + 15u) / 16u, blocks = (max(it.rows, it.cols) + 31u) / 32u;
+    const uint32_t parts = min(blocks, (uint32_t)kWholeWaves);
+    half8 xh[kWholeBlocks][2 * NB], xl[kWholeBlocks][2 * NB];
+    {
+        float v[kWholeBlocks][2 * NB][8];
+        double s;
+        if (c.step) s = c.in_type == 0 ? whole_load<NB, float, true>(c, it, blocks, wave, lane, v) : c.in_type == 1 ? whole_load<NB, Bf16, true>(c, it, blocks, wave, lane, v) : whole_load<NB, F16, true>(c, it, blocks, wave, lane, v);
+        else s = c.in_type == 0 ? whole_load<NB, float, false>(c, it, blocks, wave, lane, v) : c.in_type == 1 ? whole_load<NB, Bf16, false>(c, it, blocks, wave, lane, v) : whole_load<NB, F16, false>(c, it, blocks, wave, lane, v);
+        for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+        double* sums = reinterpret_cast<double*>(lds);
+        if (lane == 0) sums[wave] = s;
+        __syncthreads();
+        double sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < kWholeWaves; ++i) sum += sums[i];
+        __syncthreads();
+        const double norm = sqrt(sum) + (double)c.eps;
+        const double factor = norm > 0.0 ? (double)c.lift / norm : 0.0;
+#pragma unroll
+        for (int b = 0; b < kWholeBlocks; ++b)
+#pragma unroll
+            for (int k = 0; k < 2 * NB; ++k) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[b][k][e] = (float)((double)v[b][k][e] * factor);
+                split8(v[b][k], &xh[b][k], &xl[b][k]);
+            }
+    }
+    const uint8_t* p = lds + L::kP + lane * 16u;
+    half8 one[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) one[k][e] = (lane & 31u) == k * 16u + 8u * (e / 4) + 4u * (lane >> 5) + e % 4 ? (_Float16)1.f : (_Float16)0.f;
+    if (it.rows > it.cols) {
+#pragma unroll
+        for (int b = 0; b < kWholeBlocks; ++b) {
+            if (b * kWholeWaves + wave >= blocks) break;
+            half8 hi[2 * NB], lo[2 * NB];
+            whole_turn<NB>(one, xh[b], hi);
+            whole_turn<NB>(one, xl[b], lo);
+#pragma unroll
+            for (int k = 0; k < 2 * NB; ++k) {
+                xh[b][k] = hi[k];
+                xl[b][k] = lo[k];
+            }
+        }
+    }
+    float scale = 1.f;
+    for (int s = 0; s < w.steps; ++s) {
+        float16v sum[NB * (NB + 1) / 2];
+#pragma unroll
+        for (int b = 0; b < NB * (NB + 1) / 2; ++b) sum[b] = zeros();
+#pragma unroll
+        for (int b = 0; b < kWholeBlocks; ++b) {
+            if (b * kWholeWaves + wave >= blocks) break;
+            if (s) {
+                float16v acc[NB];
+                whole_times<NB, false>(p, xh[b], xl[b], steps, acc);
+                whole_split<NB>(acc, scale, xh[b], xl[b]);
+            }
+            half8 hi[2 * NB], lo[2 * NB];
+            whole_turn<NB>(one, xh[b], hi);
+            whole_turn<NB>(one, xl[b], lo);
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int i = 0, u = 0; i < NB; ++i)
+#pragma unroll
+                    for (int j = 0; j <= i; ++j, ++u) sum[u] = product3(hi[2 * i + k], lo[2 * i + k], hi[2 * j + k], lo[2 * j + k], sum[u]);
+        }
+        if (wave < parts) {
+            float4* to = reinterpret_cast<float4*>(lds) + wave * L::kUnits * 64 + lane;
+#pragma unroll
+            for (int u = 0; u < L::kUnits; ++u)
+                to[u * 64] = make_float4(sum[u / 4][u % 4 * 4], sum[u / 4][u % 4 * 4 + 1], sum[u / 4][u % 4 * 4 + 2], sum[u / 4][u % 4 * 4 + 3]);
+        }
+        __syncthreads();
+        whole_sum<NB>(lds, w.step[s].gram, parts, wave, lane);
+        __syncthreads();
+        whole_poly<NB>(lds, w.step[s], steps, wave, lane);
+        __syncthreads();
+        scale = w.step[s].apply;
+    }
+    scale *= it.gain;
+#pragma unroll
+    for (int b = 0; b < kWholeBlocks; ++b) {
+        const uint32_t bj = b * kWholeWaves + wave;
+        if (bj >= blocks) break;
+        float16v acc[NB];
+        if (it.rows > it.cols) whole_times<NB, true>(p, xh[b], xl[b], steps, acc);
+        else whole_times<NB, false>(p, xh[b], xl[b], steps, acc);
+        if (c.out_type == 0) whole_store<NB, float>(c, it, acc, scale, bj, lane);
+        else if (c.out_type == 1) whole_store<NB, Bf16>(c, it, acc, scale, bj, lane);
+        else whole_store<NB, F16>(c, it, acc, scale, bj, lane);
+    }
+}
+// ARGUMENTS: the whole list is in the launch's arguments
+template <bool ARGUMENTS>
+__global__ void __launch_bounds__(kWholeThreads, 2) k_whole(WholeArgs w, std::conditional_t<ARGUMENTS, WholeTable, NormTable<false>> table)
 {
     extern __shared__ __align__(1024) uint8_t lds[];
-    const Common& c = g.c;
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    uint32_t at;
-    const Item it = c.items[find_item(c.starts + (size_t)kChain * c.count, c.count, blockIdx.x, &at)];
-    const uint32_t nb = (it.n + 31u) / 32u;
-    if (it.chain == 2) {
-        if (nb == 1) chain_gram<1>(g, it, lds, wave, lane);
-        else chain_gram<2>(g, it, lds, wave, lane);
-    } else {
-        const Plane from{c.ws + it.square + kA * it.square_bytes, it.nf};
-        for (uint32_t i = threadIdx.x; i < nb * nb * 2u * (kFragBytes / 16u); i += kChainThreads) {
-            const uint32_t frag = i / (kFragBytes / 16u), in = i % (kFragBytes / 16u);
-            *reinterpret_cast<uint4*>(lds + i * 16u) = *reinterpret_cast<const uint4*>(from.frag(frag / (2 * nb), frag % (2 * nb)) + in * 16u);
-        }
-        __syncthreads();
-    }
-    if (nb <= 2) chain_steps<1>(g, it, lds, nb, wave, lane);
-    else chain_steps<2>(g, it, lds, nb, wave, lane);
+    MatrixSpan it;
+    if constexpr (ARGUMENTS) it = table.item[blockIdx.x];
+    else it = w.items[blockIdx.x];
+    if (min(it.rows, it.cols) <= 32) whole<1>(w, it, lds, wave, lane);
+    else whole<2>(w, it, lds, wave, lane);
 }
 
 // ---- host ----
@@ -990,21 +1132,16 @@ uint32_t norm_parts(const MatrixSpan& m)
 struct Work {
     uint32_t steps[kClasses];
     uint64_t tiles[kSizes][kClasses];
-    int chain;
 };
-// chains: every matrix of the list is short enough.  Beside longer ones, whose launches there are anyway, the short ones' tiles
-// cost nothing, and their chains would hold up the others.
-Work work_of(const MatrixSpan& m, bool chains)
+Work work_of(const MatrixSpan& m)
 {
     Work w{};
-    const uint32_t n = std::min(m.rows, m.cols), wide = std::max(m.rows, m.cols), nsteps = (n + 15) / 16, msteps = (wide + 15) / 16;
-    w.chain = !chains ? 0 : n <= kChainGram && msteps <= kChainGramSteps ? 2 : 1;
-    for (int cls = 0; cls < kClasses; ++cls) w.steps[cls] = cls == kGrams ? msteps : nsteps;
+    const uint32_t n = std::min(m.rows, m.cols), wide = std::max(m.rows, m.cols);
+    for (int cls = 0; cls < kClasses; ++cls) w.steps[cls] = ((cls == kGrams ? wide : n) + 15) / 16;
     for (int size = 0; size < kSizes; ++size) {
         const uint64_t t = kTileOf[size], nt = (n + t - 1) / t, mt = (wide + t - 1) / t, half = nt * (nt + 1) / 2;
-        w.tiles[size][kGrams] = w.chain == 2 ? 0 : half;
-        w.tiles[size][kSingles] = w.chain ? 0 : half;
-        w.tiles[size][kPairs] = w.chain ? 0 : 2 * half;
+        w.tiles[size][kGrams] = w.tiles[size][kSingles] = half;
+        w.tiles[size][kPairs] = 2 * half;
         w.tiles[size][kWides] = nt * mt;
     }
     return w;
@@ -1015,7 +1152,6 @@ Work work_of(const MatrixSpan& m, bool chains)
 constexpr double kStepUs[kSizes] = {0.12, 0.28, 1.09}, kEndsUs[kSizes] = {3.0, 5.0, 12.0}, kPutUs[kSizes - 1] = {2.0, 3.0}, kTakeUs[kSizes - 1] = {1.0, 2.0};
 constexpr uint32_t kUnits = 256;           // compute units
 constexpr uint64_t kLocalBytes = 8 << 20;  // of a matrix's operand that a launch goes through
-constexpr double kChainUs = 6.0, kChainStepUs = 5.0;
 
 Share share_of(const std::vector<Work>& work, const MatrixSpan* m, int cls, int sizes)
 {
@@ -1055,7 +1191,7 @@ Share share_of(const std::vector<Work>& work, const MatrixSpan* m, int cls, int 
 
 // Steps of a phase: one (X X^T, P, P X) or several, whichever is thought to take less.  Matrices that are about square have as
 // much work either way, and then one has fewer launches; wide ones gain from several.
-int phase_steps_of(const Share* share, bool chains, int nsteps, int most)
+int phase_steps_of(const Share* share, int nsteps, int most)
 {
     int best = 1;
     double least = 0.0;
@@ -1068,7 +1204,6 @@ int phase_steps_of(const Share* share, bool chains, int nsteps, int most)
             us += steps * share[kSingles].us;  // P
             // the first step's P A, the last one's P Q and every other's two at once; A
             if (steps > 1) us += (steps + 1) * share[kSingles].us + (steps - 2) * share[kPairs].us;
-            if (chains) us += kChainUs + steps * kChainStepUs;
         }
         if (length == 1 || us < least) {
             least = us;
@@ -1080,23 +1215,37 @@ int phase_steps_of(const Share* share, bool chains, int nsteps, int most)
 
 // How a list is taken: everything that its shapes decide.
 struct Plan {
+    bool whole;  // all matrices are small: k_whole
     std::vector<Work> work;
     Share share[kClasses];
     uint32_t room;  // rows and columns that there is room for are multiples of this
     int phase_steps;
 };
-Plan plan_of(const MatrixSpan* m, int count, int nsteps, int most_phase)
+// fine: the result is stored in 32 bits.  Then a phase has two steps only if nearly all of the list is of matrices whose own
+// sums are long enough to be as far off (n >= kFineHeight): with two steps' phases, 16 x 16, 64 x 64, 300 x 300 and 2048 x
+// 2048 are 2.8, 2.3, 2.4 and 2.7e-6 off, with one step's 0.6, 0.9, 1.5 and 3.2e-6.
+constexpr uint32_t kFineHeight = 512;
+Plan plan_of(const MatrixSpan* m, int count, int nsteps, bool fine)
 {
     Plan p{};
     uint32_t highest = 0;
-    for (int i = 0; i < count; ++i) highest = std::max(highest, std::min(m[i].rows, m[i].cols));
-    const bool chains = highest <= kChainMost;
-    p.work.reserve((size_t)count);
-    for (int i = 0; i < count; ++i) p.work.push_back(work_of(m[i], chains));
+    double values = 0, small = 0;
+    p.whole = true;
+    for (int i = 0; i < count; ++i) {
+        const uint32_t n = std::min(m[i].rows, m[i].cols), wide = std::max(m[i].rows, m[i].cols);
+        highest = std::max(highest, n);
+        p.whole = p.whole && n <= kWholeHeight && wide <= kWholeWidth && m[i].rows * m[i].stride <= kWholeExtent;
+        values += (double)n * wide;
+        if (n < kFineHeight) small += (double)n * wide;
+    }
     const int sizes = highest > Large::kTile ? kSizes : kSizes - 1;
     p.room = kTileOf[sizes - 1];
+    p.phase_steps = 1;
+    if (p.whole) return p;
+    p.work.reserve((size_t)count);
+    for (int i = 0; i < count; ++i) p.work.push_back(work_of(m[i]));
     for (int cls = 0; cls < kClasses; ++cls) p.share[cls] = share_of(p.work, m, cls, sizes);
-    p.phase_steps = phase_steps_of(p.share, chains, nsteps, most_phase);
+    p.phase_steps = phase_steps_of(p.share, nsteps, !fine ? kPhaseMost : small <= 0.1 * values ? kPhaseMost32 : 1);
     return p;
 }
 
@@ -1105,6 +1254,11 @@ template <typename Each>
 Layout lay_out(const MatrixSpan* m, int count, const Plan& plan, Each&& each)
 {
     Layout l{};
+    if (plan.whole) {
+        l.total = align256((size_t)count * sizeof(MatrixSpan));
+        l.fits = true;
+        return l;
+    }
     uint64_t sum[kKinds] = {}, sums = 0;
     for (int i = 0; i < count; ++i) sums += norm_parts(m[i]);
     size_t off = 0;
@@ -1113,7 +1267,6 @@ Layout lay_out(const MatrixSpan* m, int count, const Plan& plan, Each&& each)
     l.sums = off;   off = align256(off + sums * 8);
     bool sliced[kClasses] = {};
     for (int i = 0; i < count; ++i) {
-        const Work& w = plan.work[(size_t)i];
         Item it{};
         it.at = m[i].offset;
         it.stride = m[i].stride;
@@ -1125,7 +1278,6 @@ Layout lay_out(const MatrixSpan* m, int count, const Plan& plan, Each&& each)
         it.nf = np / 16;
         it.mf = mp / 16;
         it.gain = m[i].gain;
-        it.chain = (uint32_t)w.chain;
         const size_t x = (size_t)np * mp * 4;
         for (int k = 0; k < 2; ++k) {
             it.x[k] = off;  off += x;
@@ -1138,10 +1290,10 @@ Layout lay_out(const MatrixSpan* m, int count, const Plan& plan, Each&& each)
         uint64_t units[kKinds] = {};
         units[kNorm] = it.parts;
         units[kConvert] = (uint64_t)((it.n + 63) / 64) * ((it.m + 63) / 64);
-        units[kChain] = it.chain != 0;
         for (int cls = 0; cls < kClasses; ++cls) {
             const Share& s = plan.share[cls];
             if (!s.workgroups) continue;
+            const Work& w = plan.work[(size_t)i];
             const uint32_t slices = (w.steps[cls] + s.len - 1) / s.len;
             units[kProducts + cls] = w.tiles[s.size][cls] * slices;
             sliced[cls] = sliced[cls] || (slices > 1 && w.tiles[s.size][cls]);
@@ -1217,26 +1369,22 @@ hipError_t launch_steps(const Common& c, const OrthogonalArgs& a, const StepBoun
     int step = 0;
     for (int phase = 0; phase < b.phases && e == hipSuccess; ++phase) {
         const float lx = lift_for(b.x[phase]);
-        ChainArgs chain{};
-        chain.c = c;
-        chain.phase = phase;
         ProductArgs g{};
         g.c = c;
         g.products = 1;
         g.phase = phase;
         g.out[0] = kA;
         float la = lift_for(b.a[step]), lq = 1.f;
-        chain.gram = g.scale[0] = la / (lx * lx);
+        g.scale[0] = la / (lx * lx);
         e = launch_product<kGram>("orthogonal_gram", g, plan, places, s);
         int q = kQ0;
         for (const int first = step; step < b.end[phase] && e == hipSuccess; ++step) {
-            ChainStep& st = chain.step[chain.steps++];
             const int p = step == first ? kQ0 : kP;
             const float lp = lift_for(p == kP ? b.p[step] : std::max(b.p[step], b.q[step]));
             g.products = 1;
-            st.ca = g.ca = a.coefficients[3 * step] * lp;
-            st.cb = g.cb = a.coefficients[3 * step + 1] * lp / la;
-            st.poly = g.scale[0] = a.coefficients[3 * step + 2] * (lp / (la * la));
+            g.ca = a.coefficients[3 * step] * lp;
+            g.cb = a.coefficients[3 * step + 1] * lp / la;
+            g.scale[0] = a.coefficients[3 * step + 2] * (lp / (la * la));
             g.left[0] = g.right[0] = kA;
             g.out[0] = p;
             e = launch_product<kPoly>("orthogonal_poly", g, plan, places, s);
@@ -1247,7 +1395,7 @@ hipError_t launch_steps(const Common& c, const OrthogonalArgs& a, const StepBoun
             if (again) {  // T = P A
                 g.left[k] = p;
                 g.right[k] = kA;
-                st.t = g.scale[k] = lt / (lp * la);
+                g.scale[k] = lt / (lp * la);
                 g.out[k++] = kT;
             }
             if (p == kP) {  // Q <- P Q
@@ -1255,7 +1403,7 @@ hipError_t launch_steps(const Common& c, const OrthogonalArgs& a, const StepBoun
                 g.left[k] = kP;
                 g.right[k] = q;
                 q = q == kQ0 ? kQ1 : kQ0;
-                st.q = g.scale[k] = next / (lp * lq);
+                g.scale[k] = next / (lp * lq);
                 lq = next;
                 g.out[k++] = q;
             } else {
@@ -1268,17 +1416,11 @@ hipError_t launch_steps(const Common& c, const OrthogonalArgs& a, const StepBoun
                 g.products = 1;
                 g.left[0] = kT;
                 g.right[0] = p;
-                st.a = g.scale[0] = next / (lt * lp);
+                g.scale[0] = next / (lt * lp);
                 la = next;
                 g.out[0] = kA;
                 e = launch_product<kTimes>("orthogonal_times", g, plan, places, s);
             }
-        }
-        if (e == hipSuccess && places.count[kChain]) {
-            static std::atomic<bool> ready[64] = {};
-            chain.q = q;
-            e = allow_lds(reinterpret_cast<const void*>(&k_chain), ready, kChainLds);
-            if (e == hipSuccess) FFTSP_LAUNCH("orthogonal_chain", k_chain, dim3(places.count[kChain]), dim3(kChainThreads), kChainLds, s, chain);
         }
         if (e != hipSuccess) break;
         g.left[0] = q;
@@ -1291,6 +1433,41 @@ hipError_t launch_steps(const Common& c, const OrthogonalArgs& a, const StepBoun
         }
     }
     return e;
+}
+
+template <bool ARGUMENTS, typename Table>
+hipError_t launch_whole_list(const WholeArgs& w, const Table& table, int count, hipStream_t s)
+{
+    static std::atomic<bool> ready[64] = {};
+    const hipError_t e = allow_lds(reinterpret_cast<const void*>(&k_whole<ARGUMENTS>), ready, WholeLds<2>::kBytes);
+    if (e != hipSuccess) return e;
+    FFTSP_LAUNCH("orthogonal_whole", k_whole<ARGUMENTS>, dim3((uint32_t)count), dim3(kWholeThreads), WholeLds<2>::kBytes, s, w, table);
+    return hipGetLastError();
+}
+hipError_t launch_whole(const Common& c, const OrthogonalArgs& a, const StepBounds& b, const MatrixSpan* m, int count, hipStream_t s)
+{
+    WholeArgs w{};
+    w.c = c;
+    w.steps = a.nsteps;
+    for (int i = 0; i < a.nsteps; ++i) {
+        const float lx = lift_for(b.x[i]), la = lift_for(b.a[i]), lp = lift_for(b.p[i]);
+        w.step[i] = WholeStep{la / (lx * lx), a.coefficients[3 * i] * lp, a.coefficients[3 * i + 1] * lp / la, a.coefficients[3 * i + 2] * (lp / (la * la)),
+                              (i + 1 < a.nsteps ? lift_for(b.x[i + 1]) : 1.f) / (lp * lx)};
+    }
+    WholeTable t{};
+    if (count <= kWholeItems) {
+        std::copy(m, m + count, t.item);
+        return launch_whole_list<true>(w, t, count, s);
+    }
+    MatrixSpan* items = reinterpret_cast<MatrixSpan*>(c.ws);
+    for (int i = 0; i < count; i += kWholeItems) {
+        t.first = (uint32_t)i;
+        t.count = (uint32_t)std::min(count - i, kWholeItems);
+        std::copy(m + i, m + i + t.count, t.item);
+        FFTSP_LAUNCH("orthogonal_list", k_whole_items, dim3(1), dim3(kWholeItems), 0, s, t, items);
+    }
+    w.items = items;
+    return launch_whole_list<false>(w, NormTable<false>{}, count, s);
 }
 
 }  // namespace
@@ -1334,14 +1511,14 @@ bool step_bounds(const float* coefficients, int nsteps, int phase_steps, StepBou
 size_t orthogonal_workspace(const MatrixSpan* m, int count)
 {
     if (!count) return 0;
-    const Layout l = lay_out(m, count, plan_of(m, count, 1, 1), [](int, const Item&, const uint32_t*) {});
+    const Layout l = lay_out(m, count, plan_of(m, count, 1, false), [](int, const Item&, const uint32_t*) {});
     return l.fits ? l.total : 0;
 }
 
 hipError_t launch_orthogonal(const OrthogonalArgs& a, const MatrixSpan* m, int count, uint8_t* ws, size_t ws_bytes, bool* fits, bool* enough,
                              hipStream_t s)
 {
-    const Plan plan = plan_of(m, count, a.nsteps, a.out_type == 0 ? kPhaseMost32 : kPhaseMost);
+    const Plan plan = plan_of(m, count, a.nsteps, a.out_type == 0);
     const Layout places = lay_out(m, count, plan, [](int, const Item&, const uint32_t*) {});
     StepBounds bounds;
     if (!step_bounds(a.coefficients, a.nsteps, plan.phase_steps, &bounds)) return hipErrorInvalidValue;
@@ -1373,6 +1550,7 @@ hipError_t launch_orthogonal(const OrthogonalArgs& a, const MatrixSpan* m, int c
     c.count = (uint32_t)count;
     c.most = places.most;
     c.lift = lift_for(bounds.x[0]);
+    if (plan.whole) return launch_whole(c, a, bounds, m, count, s);
     NormTable<true> list{};
     ItemTable& t = list.t;
     t.total = (uint32_t)count;

@@ -84,6 +84,9 @@ SHAPES = {
     "long": [(5, 20011), (20011, 5)],
     "middle": [(384, 640), (640, 384)],
     "many": [(7 + 5 * i, 90 - i) for i in range(70)],
+    "small wide": [(64, 768), (768, 64), (32, 768), (767, 31), (33, 577), (513, 49), (1, 768), (17, 256)],
+    "small wider": [(64, 769), (64, 64)],
+    "small many": [(1 + i % 64, 1 + 37 * i % 768) for i in range(150)],
 }
 
 
@@ -173,6 +176,21 @@ def test_offsets_past_32_bits(dev):
     assert err <= bound + 2.0 ** -8 * 1.001 * float(torch.linalg.vector_norm(want))
 
 
+@pytest.mark.parametrize("stride", [(1 << 23) - 5, (1 << 23) + 5])   # rows from the first byte to past 2^31, and further
+def test_rows_far_apart(dev, stride):
+    torch, f = dev.torch, dev.f
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.zeros(63 * stride + 40, device="cuda")
+    m = f.Matrix(0, 64, 40, stride)
+    view(torch, x, m).copy_(matrix_like(torch, gen, 64, 40))
+    want, bound = exact(torch, view(torch, x, m))
+    listing = f.matrices([m])
+    f.orthogonal(x, x, listing, dev.workspace(f.workspace_bytes_orthogonal(listing)))
+    assert float(torch.linalg.vector_norm(view(torch, x, m).double() - want)) <= bound + 2.0 ** -24 * 1.001 * float(torch.linalg.vector_norm(want))
+    view(torch, x, m).zero_()
+    assert not bool(x.any())
+
+
 def test_ranks_sizes_and_zeros(dev):
     """a matrix of rank one, one of zeros, tiny and huge ones, eps of 0 and one that shrinks"""
     torch, f = dev.torch, dev.f
@@ -244,10 +262,11 @@ def test_a_matrix_that_is_not_finite_leaves_the_others(dev):
 @pytest.mark.parametrize("weight", ["float32", "bfloat16", "float16"])
 @pytest.mark.parametrize("grad", ["float32", "bfloat16"])
 @pytest.mark.parametrize("nesterov", [True, False])
-def test_step(dev, weight, grad, nesterov):
+@pytest.mark.parametrize("shapes", [[(16, 27), (130, 70), (64, 576), (1, 40), (200, 200)],
+                                    [(16, 27), (64, 70), (64, 576), (1, 40), (700, 50), (10, 64)]], ids=["mixed", "small"])
+def test_step(dev, weight, grad, nesterov, shapes):
     torch, f = dev.torch, dev.f
     gen = torch.Generator(device="cuda").manual_seed(8)
-    shapes = [(16, 27), (130, 70), (64, 576), (1, 40), (200, 200)]
     gains = [max(1.0, h / w) ** 0.5 for h, w in shapes]
     listing, total, ms = lay(torch, f, shapes, gains, spread=True)
     g = torch.randn(total, device="cuda", generator=gen).to(getattr(torch, grad))
