@@ -301,9 +301,10 @@ __global__ void __launch_bounds__(256) k_convert(Common c)
 
 // ---- products C = L R^T of fragments ----
 // A workgroup of WM x WN waves has a tile of 32 WM BM x 32 WN BN, a wave BM x BN blocks of 32 x 32.
-// STAGES steps of 16 along the contracted index are in LDS or on their way there.
-template <int WM_, int WN_, int BM_, int BN_, int STAGES_>
+// STAGES steps of 16 along the contracted index are in LDS or on their way there.  APART: the cross terms have sums of their own.
+template <int WM_, int WN_, int BM_, int BN_, int STAGES_, bool APART_ = false>
 struct Shape {
+    static constexpr bool APART = APART_;
     static constexpr int WM = WM_, WN = WN_, BM = BM_, BN = BN_, STAGES = STAGES_;
     static constexpr int kWaves = WM * WN, kThreads = kWaves * 64;
     static constexpr int kLeft = WM * BM, kRight = WN * BN;             // row blocks of a step
@@ -319,6 +320,9 @@ struct Shape {
 using Least = Shape<2, 2, 1, 1, 8>;  // 64 x 64
 using Small = Shape<2, 2, 2, 2, 5>;  // 128 x 128, two workgroups to a compute unit, which fill its LDS
 using Large = Shape<2, 4, 4, 2, 4>;  // 256 x 256, one
+// for results in 32 bits; Large has no registers for it
+using LeastApart = Shape<2, 2, 1, 1, 8, true>;
+using SmallApart = Shape<2, 2, 2, 2, 5, true>;
 constexpr int kSizes = 3;
 constexpr uint32_t kTileOf[kSizes] = {Least::kTile, Small::kTile, Large::kTile}, kTileBytesOf[kSizes] = {Least::kTileBytes, Small::kTileBytes, Large::kTileBytes};
 static_assert(Least::kSliced && Small::kSliced && !Large::kSliced, "the last size is not sliced");
@@ -344,7 +348,9 @@ struct Accumulators {
 // memory are issued between the products, two products apart: behind the barrier they would hold up all waves at once (at
 // 4096 x 4096 x 4096 in tiles of 256 a step of 1536 cycles of matrix instructions took 2095 that way and takes 1724, in tiles
 // of 128 two workgroups' steps 1070 and now 806 of 768; the card then lowers its clock from 1.8 to 1.6 GHz, and 1.33 and 1.20
-// PFLOP/s become 1.38 and 1.22).  idle: a wave above the diagonal of a symmetric result, which only helps to bring the pieces.
+// PFLOP/s become 1.38 and 1.22).  Results in 32 bits have sums of their own for hi lo and lo hi: each term that is added to
+// hi hi's rounds that sum once more, and five steps on 2048 x 2048 end 1.9e-6 off instead of 3.2e-6, for 1 to 3 % more time.
+// idle: a wave above the diagonal of a symmetric result, which only helps to bring the pieces.
 template <typename S>
 __device__ __forceinline__ void multiply(Accumulators<S>& acc, uint8_t* lds, const uint8_t* left, const uint8_t* right, uint64_t left_row,
                                          uint64_t right_row, uint32_t steps, bool idle, uint32_t wave, uint32_t lane)
@@ -370,6 +376,13 @@ __device__ __forceinline__ void multiply(Accumulators<S>& acc, uint8_t* lds, con
         const uint32_t rb = q / 2 < S::BN ? S::kLeft + wj + q / 2 : wi + q / 2 - S::BN;
         f[q] = *reinterpret_cast<const half8*>(lds + slot * S::kStage + rb * kFragBytes + (q & 1) * 1024u + lane * 16u);
     };
+    float16v cross[S::BM][S::BN];
+#pragma unroll
+    for (int i = 0; i < S::BM; ++i)
+#pragma unroll
+        for (int j = 0; j < S::BN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) cross[i][j][e] = 0.f;
     uint32_t slot = 0, next = S::STAGES - 1;
     auto step = [&](uint32_t k, half8 (&now)[kReads], half8 (&then)[kReads]) {
         // step k + 1 has to be there; steps k + 2 .. k + STAGES - 2 may still be on their way
@@ -382,8 +395,10 @@ __device__ __forceinline__ void multiply(Accumulators<S>& acc, uint8_t* lds, con
         for (int g = 0; g < kGroups; ++g) {
             const int t = g / S::BM, i = g % S::BM;  // hi lo, lo hi, hi hi
 #pragma unroll
-            for (int j = 0; j < S::BN; ++j)
-                acc.v[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now[2 * (S::BN + i) + (t == 1)], now[2 * j + (t == 0)], acc.v[i][j], 0, 0, 0);
+            for (int j = 0; j < S::BN; ++j) {
+                float16v& sum = S::APART && t < 2 ? cross[i][j] : acc.v[i][j];
+                sum = __builtin_amdgcn_mfma_f32_32x32x16_f16(now[2 * (S::BN + i) + (t == 1)], now[2 * j + (t == 0)], sum, 0, 0, 0);
+            }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int q = g * kAside / kGroups; q < (g + 1) * kAside / kGroups; ++q) {
@@ -421,6 +436,11 @@ __device__ __forceinline__ void multiply(Accumulators<S>& acc, uint8_t* lds, con
         step(k + 1, f[1], f[0]);
     }
     if (k < steps) step(k, f[0], f[1]);
+    if (S::APART)
+#pragma unroll
+        for (int i = 0; i < S::BM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::BN; ++j) acc.v[i][j] += cross[i][j];
     arrived<0>();  // LDS is free again
 }
 
@@ -847,6 +867,13 @@ __device__ __forceinline__ double whole_load(const Common& c, const MatrixSpan& 
     return s;
 }
 
+template <int NB, typename T>
+__device__ __forceinline__ double whole_load_of_type(const Common& c, const MatrixSpan& it, uint32_t blocks, uint32_t wave, uint32_t lane,
+                                                     float (&v)[kWholeBlocks][2 * NB][8])
+{
+    return c.step ? whole_load<NB, T, true>(c, it, blocks, wave, lane, v) : whole_load<NB, T, false>(c, it, blocks, wave, lane, v);
+}
+
 // A = scale X X^T from the waves' parts: a unit is a quarter of a block under the diagonal, which is A's both ways round
 template <int NB>
 __device__ __forceinline__ void whole_sum(uint8_t* lds, float scale, uint32_t parts, uint32_t wave, uint32_t lane)
@@ -877,7 +904,8 @@ __device__ __forceinline__ void whole_sum(uint8_t* lds, float scale, uint32_t pa
         *reinterpret_cast<half4*>(dst) = hi;
         *reinterpret_cast<half4*>(dst + 1024) = lo;
         if (i == j) continue;
-        uint8_t* to = a + (i * 2 * NB + j * 2 + col / 16) * kFragBytes + (8u * q + 4u * half + 32u * (col >> 2 & 1u)) * 16u + ((col >> 3 & 1u) * 4u + (col & 3u)) * 2u;
+        uint8_t* to = a + (i * 2 * NB + j * 2 + col / 16) * kFragBytes + (8u * q + 4u * half + 32u * (col >> 2 & 1u)) * 16u +
+                      ((col >> 3 & 1u) * 4u + (col & 3u)) * 2u;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             *reinterpret_cast<_Float16*>(to + e * 16) = hi[e];
@@ -1005,8 +1033,9 @@ __device__ __forceinline__ void whole(const WholeArgs& w, const MatrixSpan& it, 
     {
         float v[kWholeBlocks][2 * NB][8];
         double s;
-        if (c.step) s = c.in_type == 0 ? whole_load<NB, float, true>(c, it, blocks, wave, lane, v) : c.in_type == 1 ? whole_load<NB, Bf16, true>(c, it, blocks, wave, lane, v) : whole_load<NB, F16, true>(c, it, blocks, wave, lane, v);
-        else s = c.in_type == 0 ? whole_load<NB, float, false>(c, it, blocks, wave, lane, v) : c.in_type == 1 ? whole_load<NB, Bf16, false>(c, it, blocks, wave, lane, v) : whole_load<NB, F16, false>(c, it, blocks, wave, lane, v);
+        if (c.in_type == 0) s = whole_load_of_type<NB, float>(c, it, blocks, wave, lane, v);
+        else if (c.in_type == 1) s = whole_load_of_type<NB, Bf16>(c, it, blocks, wave, lane, v);
+        else s = whole_load_of_type<NB, F16>(c, it, blocks, wave, lane, v);
         for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
         double* sums = reinterpret_cast<double*>(lds);
         if (lane == 0) sums[wave] = s;
@@ -1222,8 +1251,8 @@ struct Plan {
     int phase_steps;
 };
 // fine: the result is stored in 32 bits.  Then a phase has two steps only if nearly all of the list is of matrices whose own
-// sums are long enough to be as far off (n >= kFineHeight): with two steps' phases, 16 x 16, 64 x 64, 300 x 300 and 2048 x
-// 2048 are 2.8, 2.3, 2.4 and 2.7e-6 off, with one step's 0.6, 0.9, 1.5 and 3.2e-6.
+// sums are long enough to be about as far off (n >= kFineHeight): with two steps' phases, 128 x 128, 300 x 300, 512 x 512,
+// 1024 x 1024 and 2048 x 2048 are 1.8, 1.6, 1.8, 1.7 and 1.7e-6 off, with one step's 0.9, 1.0, 1.2, 1.5 and 1.9e-6.
 constexpr uint32_t kFineHeight = 512;
 Plan plan_of(const MatrixSpan* m, int count, int nsteps, bool fine)
 {
@@ -1347,9 +1376,10 @@ hipError_t launch_product(const char* name, ProductArgs g, const Plan& plan, con
     if (workgroups == 0) return hipSuccess;
     g.len = share.len;
     g.local = share.local;
+    const bool fine = g.c.out_type == 0;
     switch (share.size) {
-        case 0: return launch_shared<Least, WHAT>(name, g, workgroups, s);
-        case 1: return launch_shared<Small, WHAT>(name, g, workgroups, s);
+        case 0: return fine ? launch_shared<LeastApart, WHAT>(name, g, workgroups, s) : launch_shared<Least, WHAT>(name, g, workgroups, s);
+        case 1: return fine ? launch_shared<SmallApart, WHAT>(name, g, workgroups, s) : launch_shared<Small, WHAT>(name, g, workgroups, s);
         default: return launch_shared<Large, WHAT>(name, g, workgroups, s);
     }
 }
