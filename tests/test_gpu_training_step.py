@@ -235,6 +235,39 @@ def test_sorted_and_sliced_calls_replay_from_a_graph(dev):
         assert torch.equal(out, want[0]) and torch.equal(y, want[1]), replay
 
 
+@pytest.mark.parametrize("count", [20, 150])   # a list that travels with the launch, and one that is written down first
+def test_steps_of_small_matrices_replay_from_a_graph(dev, count):
+    torch, f = dev.torch, dev.f
+    gen = torch.Generator(device="cuda").manual_seed(21)
+    at, ms = 0, []
+    for i in range(count):
+        rows, cols = 1 + 7 * i % 64, 1 + 61 * i % 700
+        ms.append(f.Matrix(at, *((rows, cols) if i % 2 else (cols, rows))))
+        at += rows * cols
+    listing = f.matrices(ms)
+    g, mom, w = (torch.randn(at, device="cuda", generator=gen) for _ in range(3))
+    ws = dev.workspace(f.workspace_bytes_orthogonal(listing))
+    f.orthogonal_step(g, mom.clone(), w.clone(), listing, ws, LR, BETA, DECAY)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            f.orthogonal_step(g, mom, w, listing, ws, LR, BETA, DECAY)
+    torch.cuda.synchronize()
+    for replay in range(3):
+        g.normal_(generator=gen)
+        want = mom.clone(), w.clone()
+        f.orthogonal_step(g, *want, listing, ws, LR, BETA, DECAY)
+        torch.cuda.synchronize()
+        ws.fill_(0xFF)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(mom, want[0]) and torch.equal(w, want[1]), replay
+
+
 def test_two_streams_at_once(dev):
     """each with workspaces of its own; the larger forms on both"""
     torch, f = dev.torch, dev.f
