@@ -21,6 +21,8 @@ __device__ __forceinline__ uint32_t token_row(const void* tokens, int token_bits
 }
 
 // ---- lookup: `lanes` lanes to a row (a power of two up to 256), V values to a lane at a time ----
+// Bound by bytes: 16384 rows of 2048 from fp32 into bf16, 201 MB, take 26.6 us (rows that come again are read from the caches).
+// One row of 1024 takes 1.7 us, a launch's end.
 template <typename TI, typename TO, int V, bool WHOLE>
 __global__ void __launch_bounds__(256) k_embedding(EmbeddingArgs a, uint32_t lanes)
 {
@@ -144,7 +146,8 @@ struct SortArgs {
     FillArgs fill;
 };
 
-// up to kSortOne places: one workgroup, all passes in LDS; the others fill
+// up to kSortOne places: one workgroup, all passes in LDS; the others fill.  8192 places of 64 values take 31 us with their sums, as
+// launches of many workgroups (8193) 35.  Its own work hides behind a large table's fill: 50000 x 2048 in fp32 takes 66 us, 6.2 TB/s.
 constexpr uint32_t kOneThreads = 1024, kOneWaves = kOneThreads / 64, kOneGroups = 8, kSortOne = kOneThreads * kOneGroups;
 __global__ void __launch_bounds__(kOneThreads) k_sort_one(SortArgs s)
 {
@@ -356,7 +359,8 @@ __device__ __forceinline__ void write_partial(const SumArgs& a, uint32_t stretch
     }
 }
 
-// A wave has a stretch of the sorted places and 64 V columns; kAhead rows are on their way together.
+// A wave has a stretch of the sorted places and 64 V columns; kAhead rows are on their way together.  Bound by bytes: 65536 rows
+// of 768 bf16, a third of them nobody's, and the rows of a 32000 x 768 fp32 table read and written where they have a token, 38 us.
 constexpr uint32_t kAhead = 8;
 template <typename TI, typename TO, int V, bool ADD>
 __global__ void __launch_bounds__(256) k_sum_stretches(SumArgs a, uint32_t slabs)
@@ -474,13 +478,15 @@ __global__ void __launch_bounds__(256) k_join_runs(SumArgs a)
     write_row<TO, V>(a, run, c, n, acc, there);
 }
 
-// ---- up to kFew places: no sorting, one launch ----
+// ---- up to kFew places: no sorting, one launch (700 places, 5003 x 257 in fp32: 10 us; a sort's launches take 21) ----
 // A workgroup per place and slab of 64 V columns compares its token with all others; if it is the first with that token, it sums
 // the rows of all of them, its waves eight rows at a time in turn.  Other workgroups fill the rows that no token has.
 constexpr uint32_t kFew = 2048;           // places
 constexpr uint32_t kFewRows = 1u << 18;   // rows whose bits a workgroup holds
 constexpr uint64_t kFewBytes = 32 << 20;   // of a table that is filled beside the sums
-constexpr uint64_t kFewTokens = 1u << 23;  // tokens that the workgroups read in all: 64 MB
+// workgroups that sum: some 4.5 us a thousand, where sorting takes 21 us and more.  4000 rows, bf16 into fp32: 1000, 2048 and 4096
+// workgroups (500, 1024 and 2048 places of 512 values) take 8, 12.5 and 21 us, 8000 (1000 places of 2048) 36 and by sorting 21
+constexpr uint64_t kFewGroups = 4096;
 struct FewArgs {
     EmbeddingArgs e;  // source: the rows' gradients, out: the table's
     uint32_t slabs, fillers, lanes;
@@ -617,6 +623,7 @@ uint32_t lanes_for(uint32_t width, uint32_t v)
     return lanes;
 }
 // values a lane has of a row: 16 bytes of the wider of the two types, so that a wave's accesses to either are whole lines
+// (16-bit rows into 32 bits: 5 TB/s; with 8 values, 3.2)
 constexpr int values_of(size_t in_bytes, size_t out_bytes) { return in_bytes == 4 || out_bytes == 4 ? 4 : 8; }
 
 struct GradientPlan {
@@ -684,7 +691,7 @@ hipError_t launch_embedding_gradient(const EmbeddingArgs& a, uint8_t* ws, hipStr
         return hipGetLastError();
     }
     const uint32_t in_values = values_of(type_bytes(a.source_type), type_bytes(a.out_type)), few_slabs = (a.width + 64u * in_values - 1u) / (64u * in_values);
-    if (a.ntokens <= kFew && a.ntokens * a.ntokens * few_slabs <= kFewTokens) {
+    if (a.ntokens <= kFew && a.ntokens * few_slabs <= kFewGroups) {
         // small tables are filled beside the sums, larger ones by a launch before, which writes at the memory's rate
         const bool beside = a.rows <= kFewRows && f.chunks * 16 <= kFewBytes;
         if (f.chunks && !beside) FFTSP_LAUNCH("embedding_fill", k_fill, dim3(fillers(f.chunks, 256)), dim3(256), 0, s, f);
