@@ -282,9 +282,9 @@ typedef struct fftsp_matrix {
  *   X <- a X + (b A + c A A) X with A = X X^T;   out = gain * X (transposed back).
  * coefficients: HOST array of 3 * nsteps floats, read before the call returns; NULL: five steps of
  * (3.4445, -4.7750, 2.0315), nsteps is then ignored.  1 <= nsteps <= FFTSP_MAX_STEPS.  Coefficients under which singular
- * values that begin in [0, 1] reach 4096, or their polynomials' products over three steps do, are FFTSP_EUNSUPPORTED (the
- * default: 1.3 and 41).  eps >= 0; a matrix of zeros gives zeros (with eps = 0, too).  |G|_F is taken in binary64; inside,
- * numbers have 22 bits or more and sums are binary32, whatever the types of d_in and d_out are.
+ * values s that begin in [0, 1], or a step's polynomial a + b s^2 + c s^4 of them, pass 4096 are FFTSP_EUNSUPPORTED (the
+ * default: 1.3 and 3.4), whatever the matrices are.  eps >= 0; a matrix of zeros gives zeros (with eps = 0, too).  |G|_F is
+ * taken in binary64; inside, numbers have 22 bits or more and sums are binary32, whatever the types of d_in and d_out are.
  * Every matrix is at `offset` of d_in and of d_out; d_in == d_out is allowed where the types agree, other overlaps are
  * not.  Matrices of a list must not share elements (FFTSP_EINVAL; columns of one array with one stride may alternate).
  * `matrices` is a HOST array, read before the call returns; nmat = 0 does nothing.  min(rows, cols) <= 16384,

@@ -104,7 +104,7 @@ int check_steps(OrthogonalArgs* a, const float* coefficients, int nsteps, float 
     for (int i = 0; i < 3 * a->nsteps; ++i)
         if (!std::isfinite(a->coefficients[i])) return FFTSP_EINVAL;
     StepBounds bounds;
-    return step_bounds(a->coefficients, a->nsteps, kPhaseMost, &bounds) ? FFTSP_OK : FFTSP_EUNSUPPORTED;
+    return step_bounds(a->coefficients, a->nsteps, 1, &bounds) ? FFTSP_OK : FFTSP_EUNSUPPORTED;
 }
 
 int run_orthogonal(const OrthogonalArgs& a, const fftsp_matrix* m, int count, void* ws, size_t ws_bytes, fftsp_stream_t stream)

@@ -1548,10 +1548,12 @@ size_t orthogonal_workspace(const MatrixSpan* m, int count)
 hipError_t launch_orthogonal(const OrthogonalArgs& a, const MatrixSpan* m, int count, uint8_t* ws, size_t ws_bytes, bool* fits, bool* enough,
                              hipStream_t s)
 {
-    const Plan plan = plan_of(m, count, a.nsteps, a.out_type == 0);
+    Plan plan = plan_of(m, count, a.nsteps, a.out_type == 0);
     const Layout places = lay_out(m, count, plan, [](int, const Item&, const uint32_t*) {});
+    // what is accepted does not depend on how the list is taken: where a phase's products are too large, phases are shorter
     StepBounds bounds;
-    if (!step_bounds(a.coefficients, a.nsteps, plan.phase_steps, &bounds)) return hipErrorInvalidValue;
+    while (!step_bounds(a.coefficients, a.nsteps, plan.phase_steps, &bounds))
+        if (--plan.phase_steps == 0) return hipErrorInvalidValue;  // the caller has asked about single steps
     *fits = places.fits;
     *enough = ws_bytes >= places.total;
     if (!*fits || !*enough) return hipSuccess;
