@@ -12,8 +12,8 @@
 //
 // Products run on binary16 matrix instructions whose inputs carry a binary32 number in two planes: 2^e v = hi + lo, each
 // rounded to nearest (v is then 2^-24 v off, or 2^-(25 + e) where v is small), and x y = hi hi + hi lo + lo hi summed in
-// binary32; the part left out is under 2^-24 |x| |y|.  Three instructions at sixteen times the binary32 one's rate.  e is up to
-// 14 and follows from the coefficients: they bound the singular values of every matrix of the iteration.
+// binary32; the part left out is under 2^-24 |x| |y|.  Three instructions at sixteen times the binary32 one's rate.  e is
+// 14 for values of up to one and follows from the coefficients: they bound the singular values of every matrix of the iteration.
 //
 // Layout: an operand is kept as the instruction reads it, in fragments of 32 rows x 16 columns (of the contracted index),
 // 64 lanes x 8 values of hi and then of lo: 2 KB, so that every access from memory to a wave is 1 KB in one piece, goes
@@ -1385,12 +1385,13 @@ hipError_t launch_product(const char* name, ProductArgs g, const Plan& plan, con
 }
 
 // How many times a matrix of singular values up to `bound` its planes hold: a power of two that leaves a factor of two
-// below binary16's largest number
-float lift_for(double bound)
+// below binary16's largest number, of four where the bound is a half or less
+double lift_for(double bound)
 {
     int e = 14;
     while (e > -20 && std::ldexp(bound, e) > 32768.0) --e;
-    return (float)std::ldexp(1.0, e);
+    while (e < 120 && std::ldexp(bound, e + 1) <= 16384.0) ++e;
+    return std::ldexp(1.0, e);
 }
 
 hipError_t launch_steps(const Common& c, const OrthogonalArgs& a, const StepBounds& b, const Plan& plan, const Layout& places, hipStream_t s)
@@ -1398,42 +1399,42 @@ hipError_t launch_steps(const Common& c, const OrthogonalArgs& a, const StepBoun
     hipError_t e = hipSuccess;
     int step = 0;
     for (int phase = 0; phase < b.phases && e == hipSuccess; ++phase) {
-        const float lx = lift_for(b.x[phase]);
+        const double lx = lift_for(b.x[phase]);
         ProductArgs g{};
         g.c = c;
         g.products = 1;
         g.phase = phase;
         g.out[0] = kA;
-        float la = lift_for(b.a[step]), lq = 1.f;
-        g.scale[0] = la / (lx * lx);
+        double la = lift_for(b.a[step]), lq = 1.0;
+        g.scale[0] = (float)(la / (lx * lx));
         e = launch_product<kGram>("orthogonal_gram", g, plan, places, s);
         int q = kQ0;
         for (const int first = step; step < b.end[phase] && e == hipSuccess; ++step) {
             const int p = step == first ? kQ0 : kP;
-            const float lp = lift_for(p == kP ? b.p[step] : std::max(b.p[step], b.q[step]));
+            const double lp = lift_for(p == kP ? b.p[step] : std::max(b.p[step], b.q[step]));
             g.products = 1;
-            g.ca = a.coefficients[3 * step] * lp;
-            g.cb = a.coefficients[3 * step + 1] * lp / la;
-            g.scale[0] = a.coefficients[3 * step + 2] * (lp / (la * la));
+            g.ca = (float)(a.coefficients[3 * step] * lp);
+            g.cb = (float)(a.coefficients[3 * step + 1] * lp / la);
+            g.scale[0] = (float)(a.coefficients[3 * step + 2] * (lp / (la * la)));
             g.left[0] = g.right[0] = kA;
             g.out[0] = p;
             e = launch_product<kPoly>("orthogonal_poly", g, plan, places, s);
             if (e != hipSuccess) break;
             const bool again = step + 1 < b.end[phase];
-            const float lt = lift_for(b.t[step]);
+            const double lt = lift_for(b.t[step]);
             int k = 0;
             if (again) {  // T = P A
                 g.left[k] = p;
                 g.right[k] = kA;
-                g.scale[k] = lt / (lp * la);
+                g.scale[k] = (float)(lt / (lp * la));
                 g.out[k++] = kT;
             }
             if (p == kP) {  // Q <- P Q
-                const float next = lift_for(b.q[step]);
+                const double next = lift_for(b.q[step]);
                 g.left[k] = kP;
                 g.right[k] = q;
                 q = q == kQ0 ? kQ1 : kQ0;
-                g.scale[k] = next / (lp * lq);
+                g.scale[k] = (float)(next / (lp * lq));
                 lq = next;
                 g.out[k++] = q;
             } else {
@@ -1442,11 +1443,11 @@ hipError_t launch_steps(const Common& c, const OrthogonalArgs& a, const StepBoun
             g.products = k;
             if (k) e = launch_product<kTimes>("orthogonal_times", g, plan, places, s);
             if (again && e == hipSuccess) {  // A <- T P
-                const float next = lift_for(b.a[step + 1]);
+                const double next = lift_for(b.a[step + 1]);
                 g.products = 1;
                 g.left[0] = kT;
                 g.right[0] = p;
-                g.scale[0] = next / (lt * lp);
+                g.scale[0] = (float)(next / (lt * lp));
                 la = next;
                 g.out[0] = kA;
                 e = launch_product<kTimes>("orthogonal_times", g, plan, places, s);
@@ -1455,10 +1456,10 @@ hipError_t launch_steps(const Common& c, const OrthogonalArgs& a, const StepBoun
         if (e != hipSuccess) break;
         g.left[0] = q;
         if (phase + 1 < b.phases) {
-            g.scale[0] = lift_for(b.x[phase + 1]) / (lq * lx);
+            g.scale[0] = (float)(lift_for(b.x[phase + 1]) / (lq * lx));
             e = launch_product<kApply>("orthogonal_apply", g, plan, places, s);
         } else {
-            g.scale[0] = 1.f / (lq * lx);
+            g.scale[0] = (float)(1.0 / (lq * lx));
             e = launch_product<kLast>("orthogonal_last", g, plan, places, s);
         }
     }
@@ -1480,9 +1481,9 @@ hipError_t launch_whole(const Common& c, const OrthogonalArgs& a, const StepBoun
     w.c = c;
     w.steps = a.nsteps;
     for (int i = 0; i < a.nsteps; ++i) {
-        const float lx = lift_for(b.x[i]), la = lift_for(b.a[i]), lp = lift_for(b.p[i]);
-        w.step[i] = WholeStep{la / (lx * lx), a.coefficients[3 * i] * lp, a.coefficients[3 * i + 1] * lp / la, a.coefficients[3 * i + 2] * (lp / (la * la)),
-                              (i + 1 < a.nsteps ? lift_for(b.x[i + 1]) : 1.f) / (lp * lx)};
+        const double lx = lift_for(b.x[i]), la = lift_for(b.a[i]), lp = lift_for(b.p[i]);
+        w.step[i] = WholeStep{(float)(la / (lx * lx)), (float)(a.coefficients[3 * i] * lp), (float)(a.coefficients[3 * i + 1] * lp / la),
+                              (float)(a.coefficients[3 * i + 2] * (lp / (la * la))), (float)((i + 1 < a.nsteps ? lift_for(b.x[i + 1]) : 1.0) / (lp * lx))};
     }
     WholeTable t{};
     if (count <= kWholeItems) {
@@ -1581,7 +1582,7 @@ hipError_t launch_orthogonal(const OrthogonalArgs& a, const MatrixSpan* m, int c
     c.arrivals = reinterpret_cast<uint32_t*>(ws + places.arrivals);
     c.count = (uint32_t)count;
     c.most = places.most;
-    c.lift = lift_for(bounds.x[0]);
+    c.lift = (float)lift_for(bounds.x[0]);
     if (plan.whole) return launch_whole(c, a, bounds, m, count, s);
     NormTable<true> list{};
     ItemTable& t = list.t;

@@ -21,7 +21,7 @@ def flat_list(f, shapes):
 
 
 @pytest.mark.parametrize("shapes", [[(512, 20000)], [(64, 768)], [(130, 70), (20, 2000)]], ids=lambda s: "%dx%d" % s[0])
-@pytest.mark.parametrize("factors", [(.01, 1, 1000, 5, 1), (.01, 1, 2000, 3, .5)])
+@pytest.mark.parametrize("factors", [(.01, 1, 1000, 5, 1), (.01, 1, 2000, 3, .5), (.01, .01, 100, 100, .01), (.001, 1, 60, 60, 60)])
 def test_linear_steps_scale(dev, shapes, factors):
     """X <- a X only.  A product of planes is off by 2^-23 of itself for either operand, 2^-22 for the part left out and three
     roundings of a sum that has one term, X stored by 2^-23: under 2^-20.  Five steps have at most ten products."""
