@@ -1501,42 +1501,46 @@ hipError_t launch_whole(const Common& c, const OrthogonalArgs& a, const StepBoun
     return launch_whole_list<false>(w, NormTable<false>{}, count, s);
 }
 
+// The largest magnitude of f over [0, end], where f's derivative is zero at the roots of d0 + d1 a + d2 a^2
+template <typename F>
+double largest(F&& f, double d0, double d1, double d2, double end)
+{
+    double most = std::max(std::fabs(f(0.0)), std::fabs(f(end)));
+    const double under = d1 * d1 - 4.0 * d0 * d2;
+    if (under < 0.0) return most;
+    const double r = -0.5 * (d1 + std::copysign(std::sqrt(under), d1));  // no difference of like numbers
+    for (const double at : {r / d2, d0 / r})
+        if (at > 0.0 && at < end) most = std::max(most, std::fabs(f(at)));
+    return most;
+}
+
 }  // namespace
 
-// The singular values of X, A, P, T = P A and the phase's Q, from a grid over those that X can begin with.
+// The singular values of X, A, P, T = P A and the phase's Q.  X's begin anywhere in [0, 1], and a step takes [0, top] to what the
+// odd polynomial x p(x^2) reaches there: its largest magnitude is at an end or where the derivative is zero, and so are those
+// of p(a) and a p(a) over [0, top^2].  Q's bound is the product of its steps' (the default's is reached, at zero).
 bool step_bounds(const float* coefficients, int nsteps, int phase_steps, StepBounds* b)
 {
-    constexpr int kGrid = 256;
-    double x[kGrid + 1], q[kGrid + 1];
-    for (int i = 0; i <= kGrid; ++i) x[i] = (double)i / kGrid;
+    double top = 1.0;
     b->phases = (nsteps + phase_steps - 1) / phase_steps;
     int step = 0;
     for (int phase = 0; phase < b->phases; ++phase) {
         b->end[phase] = (nsteps * (phase + 1) + b->phases - 1) / b->phases;
-        b->x[phase] = 0.0;
-        for (int i = 0; i <= kGrid; ++i) {
-            q[i] = 1.0;
-            b->x[phase] = std::max(b->x[phase], std::fabs(x[i]));
-        }
+        b->x[phase] = top;
+        double q = 1.0;
         for (; step < b->end[phase]; ++step) {
-            const double ca = coefficients[3 * step], cb = coefficients[3 * step + 1], cc = coefficients[3 * step + 2];
-            b->a[step] = b->p[step] = b->t[step] = b->q[step] = 0.0;
-            for (int i = 0; i <= kGrid; ++i) {
-                const double a = x[i] * x[i], p = ca + a * (cb + a * cc);
-                q[i] *= p;
-                x[i] *= p;
-                b->a[step] = std::max(b->a[step], a);
-                b->p[step] = std::max(b->p[step], std::fabs(p));
-                b->t[step] = std::max(b->t[step], std::fabs(a * p));
-                b->q[step] = std::max(b->q[step], std::fabs(q[i]));
-            }
-            const double most = std::max(std::max(b->a[step], b->p[step]), std::max(b->t[step], b->q[step]));
-            if (!(most <= kMostBound)) return false;
+            const double ca = coefficients[3 * step], cb = coefficients[3 * step + 1], cc = coefficients[3 * step + 2], end = top * top;
+            auto p = [&](double a) { return ca + a * (cb + a * cc); };
+            b->a[step] = end;
+            b->p[step] = largest(p, cb, 2.0 * cc, 0.0, end);
+            b->t[step] = largest([&](double a) { return a * p(a); }, ca, 2.0 * cb, 3.0 * cc, end);
+            q *= b->p[step];
+            b->q[step] = q;
+            top = largest([&](double a) { return std::sqrt(a) * p(a); }, ca, 3.0 * cb, 5.0 * cc, end);
+            if (!(std::max(end, std::max(b->t[step], q)) <= kMostBound)) return false;
         }
     }
-    for (int i = 0; i <= kGrid; ++i)
-        if (!(std::fabs(x[i]) <= kMostBound)) return false;
-    return true;
+    return top <= kMostBound;
 }
 
 size_t orthogonal_workspace(const MatrixSpan* m, int count)

@@ -2,6 +2,7 @@
 import pytest
 
 from tests.gpu_harness import Device
+from tests.newton_schulz_model import iterate, predicted
 from tests.test_gpu_orthogonal import view
 
 pytestmark = pytest.mark.gpu
@@ -40,3 +41,30 @@ def test_linear_steps_scale(dev, shapes, factors):
         want = g * (size / float(torch.linalg.vector_norm(g)))
         err = float(torch.linalg.vector_norm(view(torch, got, m).double() - want))
         assert err <= 10 * 2.0 ** -20 * size, (m.rows, m.cols, err / size)
+
+
+@pytest.mark.parametrize("shape", [(96, 200), (64, 200), (200, 40), (520, 3000)], ids=lambda s: "%dx%d" % s)
+@pytest.mark.parametrize("out", ["float32", "float16"])
+def test_steps_that_are_largest_at_small_singular_values(dev, shape, out):
+    """Nine steps take all singular values from 1/256 on to one, where the last step's polynomial is one; a smaller one meets
+    its largest, eleven.  Allowed: three times what the arithmetic's model is off, over one to three steps a phase, and half
+    a step of the result's type."""
+    torch, f = dev.torch, dev.f
+    co = [(3.4445, -4.7750, 2.0315)] * 5 + [(1.875, -1.25, 0.375)] * 4 + [(1.0, 40.0, -40.0)]
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    n = min(shape)
+    left = torch.linalg.qr(torch.randn(shape[0], n, device="cuda", generator=gen, dtype=torch.float64))[0]
+    right = torch.linalg.qr(torch.randn(shape[1], n, device="cuda", generator=gen, dtype=torch.float64))[0]
+    g = ((left * torch.logspace(0, -5, n, device="cuda", dtype=torch.float64)) @ right.t().contiguous()).float()
+    before = torch.linalg.svdvals(iterate(torch, g, co[:-1], 0.0))
+    assert float((1 + 40 * before ** 2 - 40 * before ** 4).max()) > 8    # the matrix has such a singular value
+    listing = f.matrices([f.Matrix(0, *shape)])
+    got = torch.full(shape, float("nan"), device="cuda", dtype=getattr(torch, out))
+    f.orthogonal(g.view(-1), got.view(-1), listing, dev.workspace(f.workspace_bytes_orthogonal(listing)), coefficients=co, eps=0.0)
+    off = 0.0
+    for phase in (1, 2, 3):
+        want, more = predicted(torch, g, co, 0.0, phase=phase, roundings=3)
+        off = max(off, more)
+    size = float(torch.linalg.vector_norm(want))
+    err = float(torch.linalg.vector_norm(got.double() - want))
+    assert err <= 3 * off + torch.finfo(got.dtype).eps / 2 * 1.001 * size, (err, off, size)

@@ -46,3 +46,19 @@ SHAPES = [[(64, 768)], [(65, 65)], [(300, 20000)], [(512, 20000)], [(1024, 1024)
 def test_products_over_several_steps_refuse_nothing(lib, shapes, out_type, coefficients):
     """the steps' polynomials grow past 4096 together, in one place or another, while singular values do not"""
     assert refusal(lib, shapes, coefficients, out_type) == EWORKSPACE
+
+
+USUAL = [(3.4445, -4.7750, 2.0315)] * 5
+NEAR_ONE = USUAL + [(1.875, -1.25, 0.375)] * 4      # singular values from 1/256 on are at one, smaller ones anywhere below
+
+
+def test_singular_values_between_any_samples_count(lib):
+    """x (1 + 40000 x^2 - 40000 x^4) is one at one, and 7436 where x^2 is 0.6"""
+    for shapes in ([(96, 200)], [(64, 64)], [(512, 20000)]):
+        assert refusal(lib, shapes, NEAR_ONE + [(1.0, 40000.0, -40000.0)]) == EUNSUPPORTED
+        assert refusal(lib, shapes, NEAR_ONE + [(1.0, 40.0, -40.0)]) == EWORKSPACE
+        assert refusal(lib, shapes, [(1.0, 0.0, 0.0), (0.0, 0.0, 0.0)] + USUAL) == EWORKSPACE
+        assert refusal(lib, shapes, [(0.0, 0.0, 4000.0)]) == EWORKSPACE
+        assert refusal(lib, shapes, [(0.0, 0.0, 4100.0)]) == EUNSUPPORTED
+        assert refusal(lib, shapes, [(0.0, 16000.0, -16000.0)]) == EWORKSPACE      # s p(s^2) is 2974 at s^2 = 0.6, p(s^2) 4000 at 0.5
+        assert refusal(lib, shapes, [(0.0, 16500.0, -16500.0)]) == EUNSUPPORTED    # 4125 at 0.5
