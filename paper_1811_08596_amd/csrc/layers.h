@@ -84,12 +84,12 @@ hipError_t launch_embedding_gradient(const EmbeddingArgs& a, uint8_t* ws, hipStr
 // orthogonal.hip
 constexpr int kPhaseMost = 3, kPhaseMost32 = 2;  // steps that are taken on n x n matrices before X is, for results in 16 and in 32 bits
 constexpr int kMostSteps = 16;
-constexpr double kMostBound = 4096.0;  // of a matrix's singular values anywhere in the iteration
+constexpr double kMostBound = 4096.0;  // of X's singular values and of a phase's polynomials of them
 struct StepBounds {                   // largest singular values: X before each phase; A, P, P A, and the phase's product of P, by step
     int phases, end[kMostSteps];
     double x[kMostSteps], a[kMostSteps], p[kMostSteps], t[kMostSteps], q[kMostSteps];
 };
-// false: some are larger than kMostBound
+// false: X's or a phase's are larger than kMostBound
 bool step_bounds(const float* coefficients, int nsteps, int phase_steps, StepBounds* b);
 
 struct OrthogonalArgs {

@@ -1389,7 +1389,7 @@ hipError_t launch_product(const char* name, ProductArgs g, const Plan& plan, con
 double lift_for(double bound)
 {
     int e = 14;
-    while (e > -20 && std::ldexp(bound, e) > 32768.0) --e;
+    while (std::ldexp(bound, e) > 32768.0) --e;
     while (e < 120 && std::ldexp(bound, e + 1) <= 16384.0) ++e;
     return std::ldexp(1.0, e);
 }
@@ -1537,10 +1537,10 @@ bool step_bounds(const float* coefficients, int nsteps, int phase_steps, StepBou
             q *= b->p[step];
             b->q[step] = q;
             top = largest([&](double a) { return std::sqrt(a) * p(a); }, ca, 3.0 * cb, 5.0 * cc, end);
-            if (!(std::max(end, std::max(b->t[step], q)) <= kMostBound)) return false;
+            if (!(std::max(top, q) <= kMostBound)) return false;  // A's are up to its square and T's to its cube
         }
     }
-    return top <= kMostBound;
+    return true;
 }
 
 size_t orthogonal_workspace(const MatrixSpan* m, int count)

@@ -68,3 +68,24 @@ def test_steps_that_are_largest_at_small_singular_values(dev, shape, out):
     size = float(torch.linalg.vector_norm(want))
     err = float(torch.linalg.vector_norm(got.double() - want))
     assert err <= 3 * off + torch.finfo(got.dtype).eps / 2 * 1.001 * size, (err, off, size)
+
+
+@pytest.mark.parametrize("shape", [(64, 300), (70, 300), (520, 1500)], ids=lambda s: "%dx%d" % s)
+@pytest.mark.parametrize("coefficients", [[(100, 0, 0), (.01, 0, 0)], [(3000, 0, 0), (1, -1.5e-7, 1e-14), (.5, 0, 0)],
+                                          [(40, 0, 0), (60, 0, 0), (1.6, -2e-7, 1e-14), (1, 0, 0), (1e-3, 0, 0)]])
+@pytest.mark.parametrize("out", ["float32", "bfloat16"])
+def test_singular_values_of_thousands(dev, shape, coefficients, out):
+    """Allowed: as above"""
+    torch, f = dev.torch, dev.f
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    g = torch.randn(shape, device="cuda", generator=gen) @ torch.diag(torch.logspace(0, -2, shape[1], device="cuda"))
+    listing = f.matrices([f.Matrix(0, *shape)])
+    got = torch.full(shape, float("nan"), device="cuda", dtype=getattr(torch, out))
+    f.orthogonal(g.view(-1), got.view(-1), listing, dev.workspace(f.workspace_bytes_orthogonal(listing)), coefficients=coefficients, eps=0.0)
+    off = 0.0
+    for phase in (1, 2, 3):
+        want, more = predicted(torch, g, coefficients, 0.0, phase=phase, roundings=3)
+        off = max(off, more)
+    size = float(torch.linalg.vector_norm(want))
+    err = float(torch.linalg.vector_norm(got.double() - want))
+    assert err <= 3 * off + torch.finfo(got.dtype).eps / 2 * 1.001 * size, (err, off, size)

@@ -62,3 +62,14 @@ def test_singular_values_between_any_samples_count(lib):
         assert refusal(lib, shapes, [(0.0, 0.0, 4100.0)]) == EUNSUPPORTED
         assert refusal(lib, shapes, [(0.0, 16000.0, -16000.0)]) == EWORKSPACE      # s p(s^2) is 2974 at s^2 = 0.6, p(s^2) 4000 at 0.5
         assert refusal(lib, shapes, [(0.0, 16500.0, -16500.0)]) == EUNSUPPORTED    # 4125 at 0.5
+
+
+@pytest.mark.parametrize("coefficients", [[(100.0, 0, 0), (.01, 0, 0)], [(4000.0, 0, 0), (.001, 0, 0), (1, 0, 0)], [(4000.0, 0, 0), (1, 0, 0), (1, 0, 0)],
+                                          [(4000.0, 0, 0), (2e-4, 6e-11, 0)]])
+def test_singular_values_up_to_4096_are_accepted(lib, coefficients):
+    for shapes in ([(64, 768)], [(512, 20000)], [(1024, 1024)]):
+        for out_type in (0, 1):
+            assert refusal(lib, shapes, coefficients, out_type) == EWORKSPACE
+            assert refusal(lib, shapes, [(4097.0, 0, 0)] + coefficients[1:], out_type) == EUNSUPPORTED
+            assert refusal(lib, shapes, [(-4097.0, 0, 0)] + coefficients[1:], out_type) == EUNSUPPORTED
+            assert refusal(lib, shapes, [(4000.0, 0, 0), (2.0, 0, 0)], out_type) == EUNSUPPORTED
