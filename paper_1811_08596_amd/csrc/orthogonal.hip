@@ -7,8 +7,9 @@
 // That is n^2 m for A and 2 n^2 m for Q X once a phase instead of once a step, and four symmetric n x n products (n^3
 // each: only tiles on and under the diagonal are computed, and written twice) a step instead of one.  A has an absolute error
 // of 2^-24 of its largest eigenvalue, which the small eigenvalues' growth by a^2 a step turns into a relative one: 1e-6 after
-// two steps, 3.4445^4 2^-24 = 1e-5 after three, 1e-3 after five.  So a phase has one step or two where the result is stored in
-// 32 bits (plan_of), up to three where it is rounded to 16.  Lists of small matrices take none of this: k_whole.
+// two steps, up to 3.4445^4 2^-24 = 1e-5 after three, 1e-3 after five.  So a phase has up to two steps where the result is stored
+// in 32 bits, up to three where it is rounded to 16, and one where short sums would end closer (plan_of).  Lists of small
+// matrices take none of this: k_whole.
 //
 // Products run on binary16 matrix instructions whose inputs carry a binary32 number in two planes: 2^e v = hi + lo, each
 // rounded to nearest (v is then 2^-24 v off, or 2^-(25 + e) where v is small), and x y = hi hi + hi lo + lo hi summed in
@@ -317,12 +318,9 @@ struct Shape {
     static constexpr bool kSliced = kTile < 256;  // putting down and taking up parts of 256 KB costs more than it gains
     static_assert(kLeft == kRight && (kLeft + kRight) * 2 % kWaves == 0 && kPieces * (STAGES - 2) < 64 && STAGES >= 3, "");
 };
-using Least = Shape<2, 2, 1, 1, 8>;  // 64 x 64
-using Small = Shape<2, 2, 2, 2, 5>;  // 128 x 128, two workgroups to a compute unit, which fill its LDS
-using Large = Shape<2, 4, 4, 2, 4>;  // 256 x 256, one
-// for results in 32 bits; Large has no registers for it
-using LeastApart = Shape<2, 2, 1, 1, 8, true>;
-using SmallApart = Shape<2, 2, 2, 2, 5, true>;
+using Least = Shape<2, 2, 1, 1, 8, true>;  // 64 x 64
+using Small = Shape<2, 2, 2, 2, 5, true>;  // 128 x 128, two workgroups to a compute unit, which fill its LDS
+using Large = Shape<2, 4, 4, 2, 4>;        // 256 x 256, one; no registers for sums apart
 constexpr int kSizes = 3;
 constexpr uint32_t kTileOf[kSizes] = {Least::kTile, Small::kTile, Large::kTile}, kTileBytesOf[kSizes] = {Least::kTileBytes, Small::kTileBytes, Large::kTileBytes};
 static_assert(Least::kSliced && Small::kSliced && !Large::kSliced, "the last size is not sliced");
@@ -348,7 +346,7 @@ struct Accumulators {
 // memory are issued between the products, two products apart: behind the barrier they would hold up all waves at once (at
 // 4096 x 4096 x 4096 in tiles of 256 a step of 1536 cycles of matrix instructions took 2095 that way and takes 1724, in tiles
 // of 128 two workgroups' steps 1070 and now 806 of 768; the card then lowers its clock from 1.8 to 1.6 GHz, and 1.33 and 1.20
-// PFLOP/s become 1.38 and 1.22).  Results in 32 bits have sums of their own for hi lo and lo hi: each term that is added to
+// PFLOP/s become 1.38 and 1.22).  Tiles of 64 and 128 have sums of their own for hi lo and lo hi: each term that is added to
 // hi hi's rounds that sum once more, and five steps on 2048 x 2048 end 1.9e-6 off instead of 3.2e-6, for 1 to 3 % more time.
 // idle: a wave above the diagonal of a symmetric result, which only helps to bring the pieces.
 template <typename S>
@@ -1250,10 +1248,14 @@ struct Plan {
     uint32_t room;  // rows and columns that there is room for are multiples of this
     int phase_steps;
 };
-// fine: the result is stored in 32 bits.  Then a phase has two steps only if nearly all of the list is of matrices whose own
-// sums are long enough to be about as far off (n >= kFineHeight): with two steps' phases, 128 x 128, 300 x 300, 512 x 512,
-// 1024 x 1024 and 2048 x 2048 are 1.8, 1.6, 1.8, 1.7 and 1.7e-6 off, with one step's 0.9, 1.0, 1.2, 1.5 and 1.9e-6.
+// A phase has several steps only if nearly all of the list is of matrices whose own sums are long enough to be about as far off
+// (n >= kFineHeight): in 32 bits, with phases of two steps, 128 x 128, 300 x 300, 512 x 512, 1024 x 1024 and 2048 x 2048 are 1.8,
+// 1.6, 1.8, 1.7 and 1.7e-6 off, with one step's 0.9, 1.0, 1.2, 1.5 and 1.9e-6.  Results in 16 bits have up to three steps there:
+// of 1024 x 4096 values 0.8 % are not the nearest binary16 numbers to the exact ones, of plain binary32 products' results
+// 1.2 %.  With three steps below kFineHeight, 100 x 8000 has 1.4 % and, with one large singular value, 6.8 % of them, with one
+// step 0.25 and 0.84 %, plain products 0.36 and 1.2 %; ResNet-50's list, most of it under that height, takes 0.92 and 1.21 ms.
 constexpr uint32_t kFineHeight = 512;
+// fine: the result is stored in 32 bits
 Plan plan_of(const MatrixSpan* m, int count, int nsteps, bool fine)
 {
     Plan p{};
@@ -1274,7 +1276,7 @@ Plan plan_of(const MatrixSpan* m, int count, int nsteps, bool fine)
     p.work.reserve((size_t)count);
     for (int i = 0; i < count; ++i) p.work.push_back(work_of(m[i]));
     for (int cls = 0; cls < kClasses; ++cls) p.share[cls] = share_of(p.work, m, cls, sizes);
-    p.phase_steps = phase_steps_of(p.share, nsteps, !fine ? kPhaseMost : small <= 0.1 * values ? kPhaseMost32 : 1);
+    p.phase_steps = phase_steps_of(p.share, nsteps, small > 0.1 * values ? 1 : fine ? kPhaseMost32 : kPhaseMost);
     return p;
 }
 
@@ -1376,10 +1378,9 @@ hipError_t launch_product(const char* name, ProductArgs g, const Plan& plan, con
     if (workgroups == 0) return hipSuccess;
     g.len = share.len;
     g.local = share.local;
-    const bool fine = g.c.out_type == 0;
     switch (share.size) {
-        case 0: return fine ? launch_shared<LeastApart, WHAT>(name, g, workgroups, s) : launch_shared<Least, WHAT>(name, g, workgroups, s);
-        case 1: return fine ? launch_shared<SmallApart, WHAT>(name, g, workgroups, s) : launch_shared<Small, WHAT>(name, g, workgroups, s);
+        case 0: return launch_shared<Least, WHAT>(name, g, workgroups, s);
+        case 1: return launch_shared<Small, WHAT>(name, g, workgroups, s);
         default: return launch_shared<Large, WHAT>(name, g, workgroups, s);
     }
 }

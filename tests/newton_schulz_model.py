@@ -66,3 +66,23 @@ def predicted(torch, g, coefficients, eps=1e-7, seeds=2, **how):
         gen = torch.Generator(device=g.device).manual_seed(seed)
         off = max(off, float(torch.linalg.vector_norm(iterate(torch, g, coefficients, eps, gen, **how) - want)))
     return want, off
+
+
+def allowed(torch, g, coefficients, eps=1e-7, phases=(1,), roundings=1):
+    """(the exact result, how far off the kernels' may be): twice what the model is off, and eight roundings of the result's
+    size, for matrices so small that a few draws say little"""
+    off, seeds = 0.0, 8 if g.numel() < 1000 else 2
+    for phase in phases:
+        want, more = predicted(torch, g, coefficients, eps, seeds, phase=phase, roundings=roundings)
+        off = max(off, more)
+    return want, 2 * off + 8 * 2.0 ** -24 * float(torch.linalg.vector_norm(want))
+
+
+def share_allowed(torch, g, coefficients, dtype, phases=(1,), roundings=1, gain=1.0):
+    """(the nearest numbers of a 16-bit type to the exact result, what share of a result may be others): twice the model's"""
+    near, share = (iterate(torch, g, coefficients) * gain).to(dtype), 0.0
+    for phase in phases:
+        gen = torch.Generator(device=g.device).manual_seed(phase)
+        drawn = (iterate(torch, g, coefficients, gen=gen, phase=phase, roundings=roundings) * gain).to(dtype)
+        share = max(share, float((drawn != near).double().mean()))
+    return near, 2 * share + 8 / g.numel()

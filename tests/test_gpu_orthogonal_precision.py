@@ -1,0 +1,82 @@
+"""How many bits the orthogonalised update has: results against the exact ones, with what a model of the arithmetic allows
+(newton_schulz_model, which says where its figures come from).  Matrices that products are shared among have phases of one
+step where nearly a tenth of the list's values or more is of matrices under 512 rows, of up to two above for results in 32
+bits, three in 16."""
+import pytest
+
+from tests.gpu_harness import Device
+from tests.newton_schulz_model import allowed, share_allowed
+from tests.test_gpu_orthogonal import DEFAULT, LARGE, SHAPES, lay, matrix_like, view
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def dev():
+    return Device()
+
+
+def falling(torch, gen, h, w):
+    """a few outer products of falling size, and noise"""
+    r = max(1, min(h, w) // 8)
+    size = torch.arange(1, r + 1, device="cuda", dtype=torch.float32) ** -0.7
+    return (torch.randn(h, r, device="cuda", generator=gen) * size) @ torch.randn(r, w, device="cuda", generator=gen) \
+        + 0.5 * torch.randn(h, w, device="cuda", generator=gen)
+
+
+def one_large(torch, gen, h, w):
+    """one singular value far above the others"""
+    return torch.randn(h, w, device="cuda", generator=gen) \
+        + 30 * torch.randn(h, 1, device="cuda", generator=gen) @ torch.randn(1, w, device="cuda", generator=gen)
+
+
+def low(shapes):
+    """whether a tenth of the values or more are of matrices under 512 rows"""
+    values = sum(h * w for h, w in shapes)
+    return sum(h * w for h, w in shapes if min(h, w) < 512) > 0.1 * values
+
+
+@pytest.mark.parametrize("name", list(SHAPES) + list(LARGE))
+def test_results_in_32_bits(dev, name):
+    torch, f = dev.torch, dev.f
+    shapes = SHAPES.get(name) or LARGE[name]
+    gen = torch.Generator(device="cuda").manual_seed(31)
+    listing, total, ms = lay(torch, f, shapes, [1.0] * len(shapes))
+    x = torch.zeros(total, device="cuda")
+    for m in ms:
+        view(torch, x, m).copy_(matrix_like(torch, gen, m.rows, m.cols))
+    got = torch.full_like(x, -7.0)
+    ws = dev.workspace(f.workspace_bytes_orthogonal(listing))
+    f.orthogonal(x, got, listing, ws)
+    again = torch.full_like(x, -7.0)
+    ws.fill_(0x5A)
+    f.orthogonal(x, again, listing, ws)
+    assert torch.equal(again, got)                      # every matrix, the last one's end and what is behind it
+    for m in ms[:1] if len(set(shapes)) == 1 else ms:
+        # tiles of 256 add the cross terms to the same sum
+        want, off = allowed(torch, view(torch, x, m), DEFAULT, phases=(1,) if low(shapes) else (1, 2), roundings=3 if max(min(s) for s in shapes) > 256 else 1)
+        err = float(torch.linalg.vector_norm(view(torch, got, m).double() - want))
+        assert err <= off, (m.rows, m.cols, err / float(torch.linalg.vector_norm(want)), off / float(torch.linalg.vector_norm(want)))
+
+
+@pytest.mark.parametrize("kind", ["falling", "one_large"])
+@pytest.mark.parametrize("shapes", [[(100, 8000)], [(8000, 100)], [(256, 4608)], [(64, 769)], [(64, 768)], [(193, 317)] * 2, [(1024, 4096)],
+                                    [(1024, 4096), (100, 4700)], [(100, 4700), (1024, 4096), (16, 300)]],
+                         ids=lambda s: "%d of %dx%d" % (len(s), *s[0]))
+@pytest.mark.parametrize("kept", ["float16", "bfloat16"])
+def test_results_in_16_bits(dev, kind, shapes, kept):
+    """Nearly all of them are the nearest numbers to the exact result: as many as binary32 arithmetic gives"""
+    torch, f = dev.torch, dev.f
+    gen = torch.Generator(device="cuda").manual_seed(32)
+    make = falling if kind == "falling" else one_large
+    listing, total, ms = lay(torch, f, shapes, [1.25] * len(shapes))
+    x = torch.zeros(total, device="cuda", dtype=getattr(torch, kept))
+    for m in ms:
+        view(torch, x, m).copy_(make(torch, gen, m.rows, m.cols))
+    got = torch.full_like(x, -7.0)
+    f.orthogonal(x, got, listing, dev.workspace(f.workspace_bytes_orthogonal(listing)))
+    for m in ms:
+        near, share = share_allowed(torch, view(torch, x, m), DEFAULT, x.dtype, phases=(1,) if low(shapes) else (1, 2, 3),
+                                    roundings=3 if max(min(s) for s in shapes) > 256 else 1, gain=m.gain)
+        other = float((view(torch, got, m) != near).double().mean())
+        assert other <= share, (m.rows, m.cols, other, share)
