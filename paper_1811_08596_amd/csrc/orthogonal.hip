@@ -12,15 +12,20 @@
 // matrices take none of this: k_whole.
 //
 // Products run on binary16 matrix instructions whose inputs carry a binary32 number in two planes: 2^e v = hi + lo, each
-// rounded to nearest (v is then 2^-24 v off, or 2^-(25 + e) where v is small), and x y = hi hi + hi lo + lo hi summed in
-// binary32; the part left out is under 2^-24 |x| |y|.  Three instructions at sixteen times the binary32 one's rate.  e is
-// 14 for values of up to one and follows from the coefficients: they bound the singular values of every matrix of the iteration.
+// rounded to nearest, and x y = hi hi + hi lo + lo hi summed in binary32.  For v in [1, 2) hi is up to 2^-11 off, so lo has steps
+// of up to 2^-22 and is 2^-23 off: that is v's error relative to it, or 2^-(25 + e) where v is small (binary16's least number).  The
+// part left out is up to 2^-22 |x| |y|.  Both have random signs, and a result's error is the sums' roundings as much as theirs.
+// Three instructions at sixteen times the binary32 one's rate.  e is 14 where the largest value is a half to two, and
+// follows from the coefficients: they bound the singular values of every matrix of the iteration.
 //
 // Layout: an operand is kept as the instruction reads it, in fragments of 32 rows x 16 columns (of the contracted index),
 // 64 lanes x 8 values of hi and then of lo: 2 KB, so that every access from memory to a wave is 1 KB in one piece, goes
 // straight into LDS and is read from there without conflicts.  Fragments along the contracted index follow each other.
-// X is kept twice, by rows (for X X^T) and by columns (for Q X).  Rows and columns are padded with zeros to whole tiles;
-// products of them are zero again, so no kernel asks where a matrix ends but those that read the input or write the output.
+// X is kept twice, by rows (for X X^T) and by columns (for Q X).  Its rows and columns are zero up to a multiple of 64 (what
+// k_convert writes); behind that, to the end of a tile of 128 or 256, is what the workspace held.  Products are contracted over
+// whole steps of 16, so within the zeros, which stay zero (P has a on the diagonal there, and meets zeros of A, Q and X), and a row or
+// column behind them reaches the same row or column of a product only, which nothing contracts or writes out.  So no kernel
+// asks where a matrix ends but those that read the input or write the output, as long as no contraction goes further than that.
 #include "layers.h"
 
 #include <algorithm>
