@@ -288,7 +288,8 @@ typedef struct fftsp_matrix {
  * Every matrix is at `offset` of d_in and of d_out; d_in == d_out is allowed where the types agree, other overlaps are
  * not.  Matrices of a list must not share elements (FFTSP_EINVAL; columns of one array with one stride may alternate).
  * `matrices` is a HOST array, read before the call returns; nmat = 0 does nothing.  min(rows, cols) <= 16384,
- * max(rows, cols) <= 2^20 (FFTSP_EUNSUPPORTED).  Non-finite values make their own matrix's output unspecified.
+ * max(rows, cols) <= 2^20, nmat <= 2^22 and at most 2^22 blocks of 64 x 64 values in all (FFTSP_EUNSUPPORTED; the largest
+ * matrix is that many).  Non-finite values make their own matrix's output unspecified.
  * The workspace holds fftsp_workspace_bytes_orthogonal(matrices, nmat) bytes (0 on invalid arguments). */
 #define FFTSP_MAX_STEPS 16
 size_t fftsp_workspace_bytes_orthogonal(const fftsp_matrix* matrices, int nmat);

@@ -1183,6 +1183,7 @@ Work work_of(const MatrixSpan& m)
 // a part down and taking one up.  By tile size.
 constexpr double kStepUs[kSizes] = {0.12, 0.28, 1.09}, kEndsUs[kSizes] = {3.0, 5.0, 12.0}, kPutUs[kSizes - 1] = {2.0, 3.0}, kTakeUs[kSizes - 1] = {1.0, 2.0};
 constexpr uint32_t kUnits = 256;           // compute units
+constexpr uint64_t kMostWorkgroups = 1 << 22;  // of a launch, with 512 threads: within 2^32
 constexpr uint64_t kLocalBytes = 8 << 20;  // of a matrix's operand that a launch goes through
 
 Share share_of(const std::vector<Work>& work, const MatrixSpan* m, int cls, int sizes)
@@ -1292,7 +1293,7 @@ Layout lay_out(const MatrixSpan* m, int count, const Plan& plan, Each&& each)
     Layout l{};
     if (plan.whole) {
         l.total = align256((size_t)count * sizeof(MatrixSpan));
-        l.fits = true;
+        l.fits = (uint64_t)count <= kMostWorkgroups;
         return l;
     }
     uint64_t sum[kKinds] = {}, sums = 0;
@@ -1338,7 +1339,7 @@ Layout lay_out(const MatrixSpan* m, int count, const Plan& plan, Each&& each)
         for (int k = 0; k < kKinds; ++k) l.count[k] = (uint32_t)(sum[k] += units[k]);
     }
     l.fits = true;
-    for (int k = 0; k < kKinds; ++k) l.fits = l.fits && sum[k] < (uint64_t)1 << 22;  // of 512 threads: within a launch's 2^32
+    for (int k = 0; k < kKinds; ++k) l.fits = l.fits && sum[k] <= kMostWorkgroups;
     size_t partial = 0;
     for (int cls = 0; cls < kClasses; ++cls) {
         if (!sliced[cls]) continue;

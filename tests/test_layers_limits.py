@@ -73,3 +73,27 @@ def test_singular_values_up_to_4096_are_accepted(lib, coefficients):
             assert refusal(lib, shapes, [(4097.0, 0, 0)] + coefficients[1:], out_type) == EUNSUPPORTED
             assert refusal(lib, shapes, [(-4097.0, 0, 0)] + coefficients[1:], out_type) == EUNSUPPORTED
             assert refusal(lib, shapes, [(4000.0, 0, 0), (2.0, 0, 0)], out_type) == EUNSUPPORTED
+
+
+def listing_of(count, rows, cols):
+    """count matrices behind each other"""
+    import numpy as np
+    kind = np.dtype([("offset", "<u8"), ("stride", "<u8"), ("rows", "<u4"), ("cols", "<u4"), ("gain", "<f4"), ("reserved", "<u4")])
+    m = np.zeros(count, kind)
+    m["offset"] = np.arange(count, dtype=np.uint64) * np.uint64(rows * cols)
+    m["stride"], m["rows"], m["cols"], m["gain"] = cols, rows, cols, 1
+    return m, m.ctypes.data_as(C.POINTER(fftsp.Matrix))
+
+
+def test_the_largest_lists(lib):
+    m, p = listing_of(1, 16384, 1 << 20)                   # both limits at once
+    assert lib.fftsp_workspace_bytes_orthogonal(p, 1) > 4 * 4 << 34
+    assert lib.fftsp_orthogonal(A, 1, B, 1, p, 1, None, 0, 1e-7, A + (1 << 50), 1 << 20, None) == EWORKSPACE
+    m, p = listing_of(2, 16384, 1 << 20)
+    assert lib.fftsp_workspace_bytes_orthogonal(p, 2) == 0
+    assert lib.fftsp_orthogonal(A, 1, A + (1 << 50), 1, p, 2, None, 0, 1e-7, A + (1 << 52), 1 << 62, None) == EUNSUPPORTED
+    m, p = listing_of((1 << 22) + 1, 1, 1)                  # small ones, a workgroup each
+    assert lib.fftsp_workspace_bytes_orthogonal(p, 1 << 22) > 0
+    assert lib.fftsp_workspace_bytes_orthogonal(p, (1 << 22) + 1) == 0
+    assert lib.fftsp_orthogonal(A, 0, B, 0, p, 1 << 22, None, 0, 1e-7, W, 1 << 20, None) == EWORKSPACE
+    assert lib.fftsp_orthogonal(A, 0, B, 0, p, (1 << 22) + 1, None, 0, 1e-7, W, 1 << 40, None) == EUNSUPPORTED
