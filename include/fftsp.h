@@ -249,8 +249,8 @@ typedef enum { FFTSP_F32 = 0, FFTSP_BF16 = 1, FFTSP_F16 = 2 } fftsp_type;
 /* d_out[t][j] = scale * d_table[token t][j], j < width, rounded once to out_type; a token outside [0, rows) (padding is
  * usually -1) gives a row of zeros.  Row v of the table begins at element v * table_stride, row t of the output at
  * t * out_stride (strides >= width; elements between width and the stride are neither read nor written).
- * token_bits: 32 or 64 (int32_t, int64_t).  ntokens = 0 does nothing.  rows, ntokens <= 2^30, width <= 2^20;
- * FFTSP_EINVAL otherwise.  d_out must not overlap the table or the tokens (FFTSP_EINVAL). */
+ * token_bits: 32 or 64 (int32_t, int64_t).  ntokens = 0 does nothing.  rows, ntokens <= 2^30, width <= 2^20, the last row
+ * at most 2^48 elements behind the first; FFTSP_EINVAL otherwise.  d_out must not overlap the table or the tokens (FFTSP_EINVAL). */
 int fftsp_embedding(const void* d_table, int table_type, size_t rows, uint32_t width, size_t table_stride,
                     const void* d_tokens, int token_bits, size_t ntokens, float scale,
                     void* d_out, int out_type, size_t out_stride, fftsp_stream_t stream);

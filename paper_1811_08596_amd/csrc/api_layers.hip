@@ -17,6 +17,7 @@ static_assert(sizeof(fftsp_matrix) == sizeof(MatrixSpan) && offsetof(fftsp_matri
               "one layout");
 
 constexpr size_t kMostStride = (size_t)1 << 40, kMostTokens = (size_t)1 << 30, kMostSorted = (size_t)1 << 24;
+constexpr uint64_t kMostElements = (uint64_t)1 << 48;  // from an array's first to its last
 constexpr uint32_t kMostShort = 16384, kMostLong = 1u << 20;
 
 bool aligned_to(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)bytes == 0; }
@@ -32,6 +33,7 @@ Span span_of(const void* p, uint64_t first, uint64_t last, int bytes)  // elemen
 bool meet(const Span& a, const Span& b) { return a.begin < b.end && b.begin < a.end; }
 
 uint64_t rows_end(size_t rows, uint32_t width, size_t stride) { return rows ? (uint64_t)(rows - 1) * stride + width : 0; }
+bool too_far(size_t rows, size_t stride) { return rows > 1 && rows - 1 > kMostElements / stride; }
 
 int check_embedding(const EmbeddingArgs& a, size_t source_rows, size_t out_rows)
 {
@@ -40,6 +42,7 @@ int check_embedding(const EmbeddingArgs& a, size_t source_rows, size_t out_rows)
     if (a.rows < 1 || a.rows > kMostRows || a.width < 1 || a.width > kMostWidth || a.ntokens > kMostTokens) return FFTSP_EINVAL;
     if (a.source_stride < a.width || a.out_stride < a.width || a.source_stride > kMostStride || a.out_stride > kMostStride)
         return FFTSP_EINVAL;
+    if (too_far(source_rows, a.source_stride) || too_far(out_rows, a.out_stride)) return FFTSP_EINVAL;
     if (!std::isfinite(a.scale)) return FFTSP_EINVAL;
     if ((source_rows && !a.source) || (out_rows && !a.out) || (a.ntokens && !a.tokens)) return FFTSP_EINVAL;
     if (!aligned_to(a.source, sb) || !aligned_to(a.out, ob) || !aligned_to(a.base, ob) || !aligned_to(a.tokens, a.token_bits / 8))
@@ -71,7 +74,7 @@ int check_matrices(const fftsp_matrix* m, int count, uint64_t* first, uint64_t* 
     *last = 0;
     for (int i = 0; i < count; ++i) {
         if (m[i].rows < 1 || m[i].cols < 1 || m[i].stride < m[i].cols || m[i].stride > kMostStride || m[i].reserved ||
-            m[i].offset > ((uint64_t)1 << 48) || !std::isfinite(m[i].gain))
+            m[i].offset > kMostElements || !std::isfinite(m[i].gain))
             return FFTSP_EINVAL;
         if (std::min(m[i].rows, m[i].cols) > kMostShort || std::max(m[i].rows, m[i].cols) > kMostLong) return FFTSP_EUNSUPPORTED;
         *first = std::min<uint64_t>(*first, m[i].offset);

@@ -97,3 +97,17 @@ def test_the_largest_lists(lib):
     assert lib.fftsp_workspace_bytes_orthogonal(p, (1 << 22) + 1) == 0
     assert lib.fftsp_orthogonal(A, 0, B, 0, p, 1 << 22, None, 0, 1e-7, W, 1 << 20, None) == EWORKSPACE
     assert lib.fftsp_orthogonal(A, 0, B, 0, p, (1 << 22) + 1, None, 0, 1e-7, W, 1 << 40, None) == EUNSUPPORTED
+
+
+def test_overlaps_of_rows_that_are_far_apart(lib):
+    """distances whose product passes 64 bits: the table's second row is beyond any memory, its first one still meets `out`"""
+    def lookup(rows, stride, out, count=2, out_stride=4):
+        return lib.fftsp_embedding(A, 0, rows, 4, stride, B, 64, count, 1.0, out, 0, out_stride, None)
+
+    def gradient(rows, stride, out, count=2, out_stride=4):
+        return lib.fftsp_embedding_gradient(A, 0, out_stride, B, 64, count, 1.0, None, out, 0, rows, 4, stride, W, 1 << 40, None)
+    far = 1 << 40
+    assert lookup((1 << 24) + 1, far, A + 16) == EINVAL and lookup(1 << 30, far, W) == EINVAL
+    assert lookup(1 << 10, far, W) == EINVAL and lookup(10, 4, W, 1 << 24, far) == EINVAL
+    assert gradient((1 << 24) + 1, far, W) == EINVAL and gradient(10, 4, W, (1 << 24) - 1, far) == EINVAL
+    assert lib.fftsp_embedding_gradient(A, 0, 4, B, 64, 2, 1.0, None, W, 0, 1 << 8, 4, far, W + (1 << 60), 0, None) == EWORKSPACE
