@@ -241,12 +241,13 @@ int fftsp_decompress_segments(const void* d_packed, size_t packed_bytes, float* 
  *
  * The embedding's gradient is the part of the flat gradient that most of whose rows are zero; the update takes the
  * flat gradient that a receiver leaves, matrix by matrix.  Unlike above, the arrays of this section need only their
- * own element's alignment (tensors of a flat gradient begin anywhere); workspaces are 16-byte aligned.  Everything
- * else is as stated at the top: device pointers, nothing allocated, nothing but launches on `stream`, same bytes for
- * the same inputs.  Element types: */
+ * own element's alignment (tensors of a flat gradient begin anywhere); workspaces are 16-byte aligned and must not
+ * overlap them.  Everything else is as stated at the top: device pointers, nothing allocated, nothing but launches on
+ * `stream`, same bytes for the same inputs.  These calls leave no status word: fftsp_device_status is for workspaces of the
+ * calls above and has nothing to read in one that a call of this section used last.  Element types: */
 typedef enum { FFTSP_F32 = 0, FFTSP_BF16 = 1, FFTSP_F16 = 2 } fftsp_type;
 
-/* d_out[t][j] = scale * d_table[token t][j], j < width, rounded once to out_type; a token outside [0, rows) (padding is
+/* d_out[t][j] = scale * d_table[token t][j], j < width, a binary32 product, then rounded to out_type; a token outside [0, rows) (padding is
  * usually -1) gives a row of zeros.  Row v of the table begins at element v * table_stride, row t of the output at
  * t * out_stride (strides >= width; elements between width and the stride are neither read nor written).
  * token_bits: 32 or 64 (int32_t, int64_t).  ntokens = 0 does nothing.  rows, ntokens <= 2^30, width <= 2^20, the last row
@@ -259,9 +260,9 @@ int fftsp_embedding(const void* d_table, int table_type, size_t rows, uint32_t w
  *   d_table_grad[v][j] = d_base[v][j] + scale * (sum over the t with token t == v of d_out_grad[t][j]),
  * d_base == NULL standing for zeros.  d_base has the type and stride of d_table_grad and is the same array (the sum is
  * added in place, and only rows that have a token are touched) or does not overlap it.  Tokens outside [0, rows) give
- * nothing.  Sums are binary32, in an order that depends on the tokens and sizes alone; one rounding to table_type.
- * Limits as above, and ntokens <= 2^24 (FFTSP_EUNSUPPORTED).  The workspace holds fftsp_workspace_bytes_embedding(...) bytes (0 on invalid arguments); ntokens = 0
- * needs none. */
+ * nothing.  Sums, their product with scale and the base's sum are binary32, in an order that depends on the tokens, types
+ * and sizes alone; then one rounding to table_type.  Limits as above, and ntokens <= 2^24 (FFTSP_EUNSUPPORTED).  The
+ * workspace holds fftsp_workspace_bytes_embedding(...) bytes (0 on invalid arguments); ntokens = 0 needs none. */
 size_t fftsp_workspace_bytes_embedding(size_t rows, uint32_t width, size_t ntokens);
 int fftsp_embedding_gradient(const void* d_out_grad, int out_type, size_t out_stride, const void* d_tokens,
                              int token_bits, size_t ntokens, float scale, const void* d_base, void* d_table_grad,
@@ -285,6 +286,10 @@ typedef struct fftsp_matrix {
  * values s that begin in [0, 1], or a step's polynomial a + b s^2 + c s^4 of them, pass 4096 are FFTSP_EUNSUPPORTED (the
  * default: 1.3 and 3.4), whatever the matrices are.  eps >= 0; a matrix of zeros gives zeros (with eps = 0, too).  |G|_F is
  * taken in binary64; inside, numbers have 22 bits or more and sums are binary32, whatever the types of d_in and d_out are.
+ * Five default steps are 0.5 to 7e-6 of the result's norm off, about as far as plain binary32 products; a result of 16 bits is
+ * rounded once more.  How the steps of a list are taken follows from all of its matrices, so a matrix in another list may
+ * come out with other last bits, within that.  (A list of matrices of up to 64 x 768 is one launch, and one larger matrix takes
+ * the whole list to launches of products, some five times as long: two calls are faster then.)
  * Every matrix is at `offset` of d_in and of d_out; d_in == d_out is allowed where the types agree, other overlaps are
  * not.  Matrices of a list must not share elements (FFTSP_EINVAL; columns of one array with one stride may alternate).
  * `matrices` is a HOST array, read before the call returns; nmat = 0 does nothing.  min(rows, cols) <= 16384,
@@ -299,7 +304,8 @@ int fftsp_orthogonal(const void* d_in, int in_type, void* d_out, int out_type, c
 
 /* The momentum step round it (Sec. 4: momentum SGD on the received gradient), for every matrix of the list:
  *   M' = beta M + G;  U = G + beta M' (nesterov != 0) or M';  O = the above of U (before its gain);
- *   W' = (1 - lr * weight_decay) W - lr * gain * O, rounded once to weight_type.
+ *   W' = (1 - lr * weight_decay) W - lr * gain * O in binary32 (1 - lr * weight_decay and its product with W are rounded), then
+ * rounded to weight_type.
  * d_grad is of grad_type (a receiver's output: FFTSP_F32), momentum is binary32.  All arrays hold the matrices at the
  * same offsets and strides; d_momentum_out may be d_momentum and d_weights_out may be d_weights (an update in place),
  * other overlaps are not allowed.  Elements outside the matrices are neither read nor written. */
