@@ -142,6 +142,7 @@ struct SortArgs {
     uint2* a;            // (token, place)
     uint2* b;
     uint32_t* counts;    // [passes][blocks][kDigits]
+    uint32_t* groups;    // [groups of kGroupBlocks blocks][kDigits] of the pass, or nullptr
     int passes;
     FillArgs fill;
 };
@@ -247,7 +248,39 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_count(SortArgs s)
     for (int p = 1; p < s.passes; ++p) s.counts[((size_t)p * s.blocks + blockIdx.x) * kDigits + tid] = 0;
 }
 
-// one pass: every workgroup finds where its digits begin from all blocks' counts, and counts the next pass's digits by the
+// Sums of rows of counts: all of them and the first `mine`
+__device__ __forceinline__ void add_rows(const uint32_t* rows, uint32_t count, uint32_t mine, uint32_t* before, uint32_t* total)
+{
+    uint32_t b = 0;
+    for (; b + 16 <= count; b += 16) {
+        uint32_t c[16];
+#pragma unroll
+        for (int u = 0; u < 16; ++u) c[u] = rows[(size_t)(b + u) * kDigits];
+#pragma unroll
+        for (int u = 0; u < 16; ++u) {
+            if (b + u < mine) *before += c[u];
+            *total += c[u];
+        }
+    }
+    for (; b < count; ++b) {
+        const uint32_t c = rows[(size_t)b * kDigits];
+        if (b < mine) *before += c;
+        *total += c;
+    }
+}
+// Many blocks: sums of kGroupBlocks blocks' counts each, so that a workgroup reads those of all groups and of its own group's
+// blocks, not of all blocks, whose bytes grow as the square of the places.  Two passes over 2^20, 2^22 and 2^24 places take
+// 84, 308 and 1169 us, with all blocks' counts in every workgroup 107, 855 and 18331; over 2^19 54 either way.
+constexpr uint32_t kGroupBlocks = 64, kManyBlocks = 256;
+__global__ void __launch_bounds__(kSortThreads) k_sort_groups(SortArgs s, int pass)
+{
+    const uint32_t first = blockIdx.x * kGroupBlocks;
+    uint32_t before = 0, total = 0;
+    add_rows(s.counts + ((size_t)pass * s.blocks + first) * kDigits + threadIdx.x, min(kGroupBlocks, s.blocks - first), 0, &before, &total);
+    s.groups[(size_t)blockIdx.x * kDigits + threadIdx.x] = total;
+}
+
+// one pass: every workgroup finds where its digits begin from the blocks' counts, and counts the next pass's digits by the
 // block that its places go to
 __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortArgs s, int pass)
 {
@@ -269,21 +302,14 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortArgs s, int p
     }
 #pragma unroll
     for (int w = 0; w < kSortWaves; ++w) wave_count[w][tid] = 0;
-    uint32_t before = 0, total = 0, b = 0;
-    for (; b + 16 <= s.blocks; b += 16) {
-        uint32_t c[16];
-#pragma unroll
-        for (int u = 0; u < 16; ++u) c[u] = counts[(size_t)(b + u) * kDigits];
-#pragma unroll
-        for (int u = 0; u < 16; ++u) {
-            if (b + u < blockIdx.x) before += c[u];
-            total += c[u];
-        }
-    }
-    for (; b < s.blocks; ++b) {
-        const uint32_t c = counts[(size_t)b * kDigits];
-        if (b < blockIdx.x) before += c;
-        total += c;
+    uint32_t before = 0, total = 0;
+    if (s.groups) {
+        const uint32_t group = blockIdx.x / kGroupBlocks;
+        uint32_t own = 0;
+        add_rows(s.groups + tid, (s.blocks + kGroupBlocks - 1) / kGroupBlocks, group, &before, &total);
+        add_rows(counts + (size_t)group * kGroupBlocks * kDigits, blockIdx.x % kGroupBlocks, kGroupBlocks, &before, &own);
+    } else {
+        add_rows(counts, s.blocks, blockIdx.x, &before, &total);
     }
     uint32_t sum = digits_before(total, scan) + before;  // a barrier within: wave_count is clear
     uint32_t rank[kGroups];
@@ -629,7 +655,7 @@ constexpr int values_of(size_t in_bytes, size_t out_bytes) { return in_bytes == 
 struct GradientPlan {
     uint32_t blocks, stretch, stretches;
     int passes;
-    size_t a, b, counts, partial, total;
+    size_t a, b, counts, groups, partial, total;
 };
 GradientPlan gradient_plan(size_t rows, uint32_t width, size_t count)
 {
@@ -644,6 +670,7 @@ GradientPlan gradient_plan(size_t rows, uint32_t width, size_t count)
     p.a = off;       off = align256(off + count * 8);
     p.b = off;       off = align256(off + count * 8);
     p.counts = off;  off = align256(off + (size_t)p.passes * p.blocks * kDigits * 4);
+    p.groups = off;  off = align256(off + (p.blocks > kManyBlocks ? (size_t)(p.blocks + kGroupBlocks - 1) / kGroupBlocks * kDigits * 4 : 0));
     p.partial = off; off = align256(off + (size_t)p.stretches * 2 * width * 4);
     p.total = off;
     return p;
@@ -714,14 +741,18 @@ hipError_t launch_embedding_gradient(const EmbeddingArgs& a, uint8_t* ws, hipStr
     }
     const GradientPlan p = gradient_plan(a.rows, a.width, a.ntokens);
     SortArgs so{a.tokens, a.token_bits, (uint32_t)a.rows, (uint32_t)a.ntokens, p.blocks, reinterpret_cast<uint2*>(ws + p.a),
-                reinterpret_cast<uint2*>(ws + p.b), reinterpret_cast<uint32_t*>(ws + p.counts), p.passes, f};
+                reinterpret_cast<uint2*>(ws + p.b), reinterpret_cast<uint32_t*>(ws + p.counts),
+                p.blocks > kManyBlocks ? reinterpret_cast<uint32_t*>(ws + p.groups) : nullptr, p.passes, f};
     const bool one = so.count <= kSortOne;
     if (one) {
         FFTSP_LAUNCH("embedding_sort_one", k_sort_one, dim3(1 + fillers(f.chunks, kOneThreads)), dim3(kOneThreads), 0, s, so);
     } else {
         const dim3 grid(p.blocks + fillers((f.chunks + p.passes) / (p.passes + 1), kSortThreads));
         FFTSP_LAUNCH("embedding_sort_count", k_sort_count, grid, dim3(kSortThreads), 0, s, so);
-        for (int i = 0; i < p.passes; ++i) FFTSP_LAUNCH("embedding_sort", k_sort_scatter, grid, dim3(kSortThreads), 0, s, so, i);
+        for (int i = 0; i < p.passes; ++i) {
+            if (so.groups) FFTSP_LAUNCH("embedding_sort_groups", k_sort_groups, dim3((p.blocks + kGroupBlocks - 1) / kGroupBlocks), dim3(kSortThreads), 0, s, so, i);
+            FFTSP_LAUNCH("embedding_sort", k_sort_scatter, grid, dim3(kSortThreads), 0, s, so, i);
+        }
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
