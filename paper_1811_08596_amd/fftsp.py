@@ -32,7 +32,11 @@ class Matrix(C.Structure):
                 ("gain", C.c_float), ("reserved", C.c_uint32)]
 
     def __init__(self, offset: int, rows: int, cols: int, stride: Optional[int] = None, gain: float = 1.0):
-        super().__init__(offset, cols if stride is None else stride, rows, cols, gain, 0)
+        stride = cols if stride is None else stride
+        # a field takes any number modulo its range
+        if not (0 <= offset < 1 << 64 and 0 <= stride < 1 << 64 and 0 <= rows < 1 << 32 and 0 <= cols < 1 << 32):
+            raise ValueError(f"no such matrix: {rows} x {cols} at {offset}, stride {stride}")
+        super().__init__(offset, stride, rows, cols, gain, 0)
 
 
 _mp = C.POINTER(Matrix)
@@ -416,6 +420,8 @@ def _rows(t, width: int):
         shape = t.shape
     rows, values = shape
     stride, one = t.stride()
+    if width >> 32:
+        raise ValueError(f"rows of {width} values are too long")
     if values != width or (width > 1 and one != 1):
         raise ValueError(f"rows of {width} consecutive values are wanted, got {tuple(shape)} with strides {t.stride()}")
     return t.data_ptr(), rows, stride if rows > 1 else max(width, stride)
@@ -443,7 +449,7 @@ def embedding(table, tokens, out, scale: float = 1.0, stream=None):
 
 
 def workspace_bytes_embedding(rows: int, width: int, ntokens: int) -> int:
-    return load().fftsp_workspace_bytes_embedding(rows, width, ntokens)
+    return 0 if width >> 32 else load().fftsp_workspace_bytes_embedding(rows, width, ntokens)
 
 
 def embedding_gradient(out_grad, tokens, table_grad, workspace, scale: float = 1.0, base=None, stream=None):

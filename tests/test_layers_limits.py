@@ -111,3 +111,16 @@ def test_overlaps_of_rows_that_are_far_apart(lib):
     assert lookup(1 << 10, far, W) == EINVAL and lookup(10, 4, W, 1 << 24, far) == EINVAL
     assert gradient((1 << 24) + 1, far, W) == EINVAL and gradient(10, 4, W, (1 << 24) - 1, far) == EINVAL
     assert lib.fftsp_embedding_gradient(A, 0, 4, B, 64, 2, 1.0, None, W, 0, 1 << 8, 4, far, W + (1 << 60), 0, None) == EWORKSPACE
+
+
+def test_the_binding_takes_no_size_modulo_a_fields_range():
+    torch = pytest.importorskip("torch")
+    for bad in ((0, (1 << 32) + 4, 1), (0, 1, (1 << 32) + 4), (-1, 4, 4), (0, -4, 4), (0, 4, -4), (1 << 64, 4, 4), (0, 4, 4, (1 << 64) + 4), (0, 4, 4, -1)):
+        with pytest.raises(ValueError):
+            fftsp.Matrix(*bad)
+    m = fftsp.Matrix(5, (1 << 32) - 1, 7, 9, 2.0)
+    assert (m.offset, m.stride, m.rows, m.cols, m.gain, m.reserved) == (5, 9, (1 << 32) - 1, 7, 2.0, 0)
+    wide = torch.empty(2, (1 << 32) + 4, device="meta", dtype=torch.float16)
+    with pytest.raises(ValueError):
+        fftsp._rows(wide, wide.shape[-1])
+    assert fftsp.workspace_bytes_embedding(10, (1 << 32) + 4, 3) == 0
