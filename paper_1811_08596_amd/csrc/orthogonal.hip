@@ -1254,26 +1254,23 @@ struct Plan {
     uint32_t room;  // rows and columns that there is room for are multiples of this
     int phase_steps;
 };
-// A phase has several steps only if nearly all of the list is of matrices whose own sums are long enough to be about as far off
-// (n >= kFineHeight): in 32 bits, with phases of two steps, 128 x 128, 300 x 300, 512 x 512, 1024 x 1024 and 2048 x 2048 are 1.8,
-// 1.6, 1.8, 1.7 and 1.7e-6 off, with one step's 0.9, 1.0, 1.2, 1.5 and 1.9e-6.  Results in 16 bits have up to three steps there:
-// of 1024 x 4096 values 0.8 % are not the nearest binary16 numbers to the exact ones, of plain binary32 products' results
-// 1.2 %.  With three steps below kFineHeight, 100 x 8000 has 1.4 % and, with one large singular value, 6.8 % of them, with one
-// step 0.25 and 0.84 %, plain products 0.36 and 1.2 %; ResNet-50's list, most of it under that height, takes 0.92 and 1.21 ms.
+// A phase has several steps only for matrices whose own sums are long enough to be about as far off (n >= kFineHeight; a list's
+// others are a part of their own, Parts): in 32 bits, with phases of two steps, 128 x 128, 300 x 300, 512 x 512, 1024 x 1024
+// and 2048 x 2048 are 1.8, 1.6, 1.8, 1.7 and 1.7e-6 off, with one step's 0.9, 1.0, 1.2, 1.5 and 1.9e-6.  Results in 16 bits have
+// up to three steps there: of 1024 x 4096 values 0.8 % are not the nearest binary16 numbers to the exact ones, of plain
+// binary32 products' results 1.2 %.  With three steps below kFineHeight, 100 x 8000 has 1.4 % and, with one large singular value,
+// 6.8 % of them, with one step 0.25 and 0.84 %, plain products 0.36 and 1.2 %.
 constexpr uint32_t kFineHeight = 512;
 // fine: the result is stored in 32 bits
 Plan plan_of(const MatrixSpan* m, int count, int nsteps, bool fine)
 {
     Plan p{};
     uint32_t highest = 0;
-    double values = 0, small = 0;
     p.whole = true;
     for (int i = 0; i < count; ++i) {
         const uint32_t n = std::min(m[i].rows, m[i].cols), wide = std::max(m[i].rows, m[i].cols);
         highest = std::max(highest, n);
         p.whole = p.whole && n <= kWholeHeight && wide <= kWholeWidth && m[i].rows * m[i].stride <= kWholeExtent;
-        values += (double)n * wide;
-        if (n < kFineHeight) small += (double)n * wide;
     }
     const int sizes = highest > Large::kTile ? kSizes : kSizes - 1;
     p.room = kTileOf[sizes - 1];
@@ -1282,7 +1279,7 @@ Plan plan_of(const MatrixSpan* m, int count, int nsteps, bool fine)
     p.work.reserve((size_t)count);
     for (int i = 0; i < count; ++i) p.work.push_back(work_of(m[i]));
     for (int cls = 0; cls < kClasses; ++cls) p.share[cls] = share_of(p.work, m, cls, sizes);
-    p.phase_steps = phase_steps_of(p.share, nsteps, small > 0.1 * values ? 1 : fine ? kPhaseMost32 : kPhaseMost);
+    p.phase_steps = phase_steps_of(p.share, nsteps, highest < kFineHeight ? 1 : fine ? kPhaseMost32 : kPhaseMost);
     return p;
 }
 
@@ -1550,25 +1547,34 @@ bool step_bounds(const float* coefficients, int nsteps, int phase_steps, StepBou
     return true;
 }
 
-size_t orthogonal_workspace(const MatrixSpan* m, int count)
-{
-    if (!count) return 0;
-    const Layout l = lay_out(m, count, plan_of(m, count, 1, false), [](int, const Item&, const uint32_t*) {});
-    return l.fits ? l.total : 0;
-}
+namespace {
 
-hipError_t launch_orthogonal(const OrthogonalArgs& a, const MatrixSpan* m, int count, uint8_t* ws, size_t ws_bytes, bool* fits, bool* enough,
-                             hipStream_t s)
+// A list's matrices under kFineHeight and the others: one part behind the other, in the same workspace.  All in one list of
+// phases of one step, ResNet-50's 54 matrices take 1257 us and so 1188; AlexNet's eight, with two steps for all, 10.83 ms and so 10.95.
+struct Parts {
+    std::vector<MatrixSpan> held;  // where there are both
+    const MatrixSpan* m[2];
+    int count[2];
+    Parts(const MatrixSpan* list, int n)
+    {
+        auto low = [](const MatrixSpan& x) { return std::min(x.rows, x.cols) < kFineHeight; };
+        count[0] = (int)std::count_if(list, list + n, low);
+        count[1] = n - count[0];
+        m[0] = m[1] = list;
+        if (!count[0] || !count[1]) return;
+        held.assign(list, list + n);
+        std::stable_partition(held.begin(), held.end(), low);
+        m[0] = held.data();
+        m[1] = held.data() + count[0];
+    }
+};
+
+hipError_t launch_part(const OrthogonalArgs& a, const MatrixSpan* m, int count, Plan plan, const Layout& places, uint8_t* ws, hipStream_t s)
 {
-    Plan plan = plan_of(m, count, a.nsteps, a.out_type == 0);
-    const Layout places = lay_out(m, count, plan, [](int, const Item&, const uint32_t*) {});
     // what is accepted does not depend on how the list is taken: where a phase's products are too large, phases are shorter
     StepBounds bounds;
     while (!step_bounds(a.coefficients, a.nsteps, plan.phase_steps, &bounds))
         if (--plan.phase_steps == 0) return hipErrorInvalidValue;  // the caller has asked about single steps
-    *fits = places.fits;
-    *enough = ws_bytes >= places.total;
-    if (!*fits || !*enough) return hipSuccess;
     Item* items = reinterpret_cast<Item*>(ws + places.items);
     uint32_t* starts = reinterpret_cast<uint32_t*>(ws + places.starts);
     Common c{};
@@ -1615,6 +1621,44 @@ hipError_t launch_orthogonal(const OrthogonalArgs& a, const MatrixSpan* m, int c
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     return launch_steps(c, a, bounds, plan, places, s);
+}
+
+}  // namespace
+
+size_t orthogonal_workspace(const MatrixSpan* m, int count)
+{
+    const Parts parts(m, count);
+    size_t most = 0;
+    for (int i = 0; i < 2; ++i) {
+        if (!parts.count[i]) continue;
+        const Layout l = lay_out(parts.m[i], parts.count[i], plan_of(parts.m[i], parts.count[i], 1, false), [](int, const Item&, const uint32_t*) {});
+        if (!l.fits) return 0;
+        most = std::max(most, l.total);
+    }
+    return most;
+}
+
+hipError_t launch_orthogonal(const OrthogonalArgs& a, const MatrixSpan* m, int count, uint8_t* ws, size_t ws_bytes, bool* fits, bool* enough,
+                             hipStream_t s)
+{
+    const Parts parts(m, count);
+    Plan plan[2];
+    Layout places[2];
+    *fits = *enough = true;
+    for (int i = 0; i < 2; ++i) {
+        if (!parts.count[i]) continue;
+        plan[i] = plan_of(parts.m[i], parts.count[i], a.nsteps, a.out_type == 0);
+        places[i] = lay_out(parts.m[i], parts.count[i], plan[i], [](int, const Item&, const uint32_t*) {});
+        *fits = *fits && places[i].fits;
+        *enough = *enough && ws_bytes >= places[i].total;
+    }
+    if (!*fits || !*enough) return hipSuccess;
+    for (int i = 0; i < 2; ++i) {
+        if (!parts.count[i]) continue;
+        const hipError_t e = launch_part(a, parts.m[i], parts.count[i], plan[i], places[i], ws, s);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace fftsp
