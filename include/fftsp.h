@@ -286,8 +286,8 @@ typedef struct fftsp_matrix {
  * values s that begin in [0, 1], or a step's polynomial a + b s^2 + c s^4 of them, pass 4096 are FFTSP_EUNSUPPORTED (the
  * default: 1.3 and 3.4), whatever the matrices are.  eps >= 0; a matrix of zeros gives zeros (with eps = 0, too).  |G|_F is
  * taken in binary64; inside, numbers have 22 bits or more and sums are binary32, whatever the types of d_in and d_out are.
- * Five default steps are 0.5 to 7e-6 of the result's norm off, about as far as plain binary32 products; a result of 16 bits is
- * rounded once more.  How products are shared out follows from the whole list, so a matrix in another list may come out with
+ * Five default steps are 0.5 to 8e-6 of the result's norm off, about as far as plain binary32 products; a result of 16 bits is
+ * the one of 32, rounded.  How products are shared out follows from the whole list, so a matrix in another list may come out with
  * other last bits, within that.  (Matrices of up to 64 x 768 are one launch if all of the list's with min(rows, cols) < 512 are that
  * small; one larger takes them to launches of products, a thousand of them for five times as long: two calls are faster then.)
  * Every matrix is at `offset` of d_in and of d_out; d_in == d_out is allowed where the types agree, other overlaps are

@@ -82,7 +82,7 @@ size_t embedding_gradient_workspace(size_t rows, uint32_t width, size_t ntokens)
 hipError_t launch_embedding_gradient(const EmbeddingArgs& a, uint8_t* ws, hipStream_t s);
 
 // orthogonal.hip
-constexpr int kPhaseMost = 3, kPhaseMost32 = 2;  // steps that are taken on n x n matrices before X is, for results in 16 and in 32 bits
+constexpr int kPhaseMost = 2;  // steps that are taken on n x n matrices before X is
 constexpr int kMostSteps = 16;
 constexpr double kMostBound = 4096.0;  // of X's singular values and of a phase's polynomials of them
 struct StepBounds {                   // largest singular values: X before each phase; A, P, P A, and the phase's product of P, by step

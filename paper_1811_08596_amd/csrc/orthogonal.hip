@@ -7,8 +7,8 @@
 // That is n^2 m for A and 2 n^2 m for Q X once a phase instead of once a step, and four symmetric n x n products (n^3
 // each: only tiles on and under the diagonal are computed, and written twice) a step instead of one.  A has an absolute error
 // of 2^-24 of its largest eigenvalue, which the small eigenvalues' growth by a^2 a step turns into a relative one: 1e-6 after
-// two steps, up to 3.4445^4 2^-24 = 1e-5 after three, 1e-3 after five.  So a phase has up to two steps where the result is stored
-// in 32 bits, up to three where it is rounded to 16, and one where short sums would end closer (plan_of).  Lists of small
+// two steps, up to 3.4445^4 2^-24 = 1e-5 after three, 1e-3 after five.  So a phase has up to two steps, and one where short sums
+// would end closer (plan_of), whatever type the result is stored in: in 16 bits it is the one in 32, rounded.  Lists of small
 // matrices take none of this: k_whole.
 //
 // Products run on binary16 matrix instructions whose inputs carry a binary32 number in two planes: 2^e v = hi + lo, each
@@ -1254,15 +1254,13 @@ struct Plan {
     uint32_t room;  // rows and columns that there is room for are multiples of this
     int phase_steps;
 };
-// A phase has several steps only for matrices whose own sums are long enough to be about as far off (n >= kFineHeight; a list's
-// others are a part of their own, Parts): in 32 bits, with phases of two steps, 128 x 128, 300 x 300, 512 x 512, 1024 x 1024
-// and 2048 x 2048 are 1.8, 1.6, 1.8, 1.7 and 1.7e-6 off, with one step's 0.9, 1.0, 1.2, 1.5 and 1.9e-6.  Results in 16 bits have
-// up to three steps there: of 1024 x 4096 values 0.8 % are not the nearest binary16 numbers to the exact ones, of plain
-// binary32 products' results 1.2 %.  With three steps below kFineHeight, 100 x 8000 has 1.4 % and, with one large singular value,
-// 6.8 % of them, with one step 0.25 and 0.84 %, plain products 0.36 and 1.2 %.
+// A phase has two steps only for matrices whose own sums are long enough to be about as far off (n >= kFineHeight; a list's
+// others are a part of their own, Parts): with phases of two steps, 128 x 128, 300 x 300, 512 x 512, 1024 x 1024 and 2048 x 2048
+// are 1.8, 1.6, 1.8, 1.7 and 1.7e-6 off, with one step's 0.9, 1.0, 1.2, 1.5 and 1.9e-6.  Three would do for no type: with them
+// 4.8 % of 8192 x 16384 random numbers' binary16 results are not the nearest to the exact ones (plain binary32 products: 2.9 %,
+// two steps: 1.5 %), and of 100 x 8000 with one large singular value 6.8 % (1.2 %, one step: 0.84 %).
 constexpr uint32_t kFineHeight = 512;
-// fine: the result is stored in 32 bits
-Plan plan_of(const MatrixSpan* m, int count, int nsteps, bool fine)
+Plan plan_of(const MatrixSpan* m, int count, int nsteps)
 {
     Plan p{};
     uint32_t highest = 0;
@@ -1279,7 +1277,7 @@ Plan plan_of(const MatrixSpan* m, int count, int nsteps, bool fine)
     p.work.reserve((size_t)count);
     for (int i = 0; i < count; ++i) p.work.push_back(work_of(m[i]));
     for (int cls = 0; cls < kClasses; ++cls) p.share[cls] = share_of(p.work, m, cls, sizes);
-    p.phase_steps = phase_steps_of(p.share, nsteps, highest < kFineHeight ? 1 : fine ? kPhaseMost32 : kPhaseMost);
+    p.phase_steps = phase_steps_of(p.share, nsteps, highest < kFineHeight ? 1 : kPhaseMost);
     return p;
 }
 
@@ -1631,7 +1629,7 @@ size_t orthogonal_workspace(const MatrixSpan* m, int count)
     size_t most = 0;
     for (int i = 0; i < 2; ++i) {
         if (!parts.count[i]) continue;
-        const Layout l = lay_out(parts.m[i], parts.count[i], plan_of(parts.m[i], parts.count[i], 1, false), [](int, const Item&, const uint32_t*) {});
+        const Layout l = lay_out(parts.m[i], parts.count[i], plan_of(parts.m[i], parts.count[i], 1), [](int, const Item&, const uint32_t*) {});
         if (!l.fits) return 0;
         most = std::max(most, l.total);
     }
@@ -1647,7 +1645,7 @@ hipError_t launch_orthogonal(const OrthogonalArgs& a, const MatrixSpan* m, int c
     *fits = *enough = true;
     for (int i = 0; i < 2; ++i) {
         if (!parts.count[i]) continue;
-        plan[i] = plan_of(parts.m[i], parts.count[i], a.nsteps, a.out_type == 0);
+        plan[i] = plan_of(parts.m[i], parts.count[i], a.nsteps);
         places[i] = lay_out(parts.m[i], parts.count[i], plan[i], [](int, const Item&, const uint32_t*) {});
         *fits = *fits && places[i].fits;
         *enough = *enough && ws_bytes >= places[i].total;

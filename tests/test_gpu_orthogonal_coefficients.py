@@ -47,7 +47,7 @@ def test_linear_steps_scale(dev, shapes, factors):
 @pytest.mark.parametrize("out", ["float32", "float16"])
 def test_steps_that_are_largest_at_small_singular_values(dev, shape, out):
     """Nine steps take all singular values from 1/256 on to one, where the last step's polynomial is one; a smaller one meets
-    its largest, eleven.  Allowed: three times what the arithmetic's model is off, over one to three steps a phase, and half
+    its largest, eleven.  Allowed: three times what the arithmetic's model is off, over one and two steps a phase, and half
     a step of the result's type."""
     torch, f = dev.torch, dev.f
     co = [(3.4445, -4.7750, 2.0315)] * 5 + [(1.875, -1.25, 0.375)] * 4 + [(1.0, 40.0, -40.0)]
@@ -62,7 +62,7 @@ def test_steps_that_are_largest_at_small_singular_values(dev, shape, out):
     got = torch.full(shape, float("nan"), device="cuda", dtype=getattr(torch, out))
     f.orthogonal(g.view(-1), got.view(-1), listing, dev.workspace(f.workspace_bytes_orthogonal(listing)), coefficients=co, eps=0.0)
     off = 0.0
-    for phase in (1, 2, 3):
+    for phase in (1, 2):
         want, more = predicted(torch, g, co, 0.0, phase=phase, roundings=3)
         off = max(off, more)
     size = float(torch.linalg.vector_norm(want))
@@ -83,7 +83,7 @@ def test_singular_values_of_thousands(dev, shape, coefficients, out):
     got = torch.full(shape, float("nan"), device="cuda", dtype=getattr(torch, out))
     f.orthogonal(g.view(-1), got.view(-1), listing, dev.workspace(f.workspace_bytes_orthogonal(listing)), coefficients=coefficients, eps=0.0)
     off = 0.0
-    for phase in (1, 2, 3):
+    for phase in (1, 2):
         want, more = predicted(torch, g, coefficients, 0.0, phase=phase, roundings=3)
         off = max(off, more)
     size = float(torch.linalg.vector_norm(want))

@@ -1,6 +1,6 @@
 """How many bits the orthogonalised update has: results against the exact ones, with what a model of the arithmetic allows
 (newton_schulz_model, which says where its figures come from).  Matrices under 512 rows have phases of one step whatever else is
-in the list, others of up to two for results in 32 bits and three in 16."""
+in the list, others of up to two; a result in 16 bits is the one in 32, rounded."""
 import pytest
 
 from tests.gpu_harness import Device
@@ -59,7 +59,7 @@ def test_results_in_32_bits(dev, name):
 @pytest.mark.parametrize("kind", ["falling", "one_large"])
 @pytest.mark.parametrize("shapes", [[(100, 8000)], [(8000, 100)], [(256, 4608)], [(64, 769)], [(64, 768)], [(193, 317)] * 2, [(1024, 4096)],
                                     [(1024, 4096), (100, 4700)], [(100, 4700), (1024, 4096), (16, 300)],
-                                    [(1024, 4096), (100, 4600)], [(16, 2000), (520, 9000), (60, 60), (3000, 60), (2000, 600)]],
+                                    [(1024, 4096), (100, 4600)], [(16, 2000), (520, 9000), (60, 60), (3000, 60), (2000, 600)], [(513, 20000)]],
                          ids=lambda s: "%d of %dx%d" % (len(s), *s[0]))
 @pytest.mark.parametrize("kept", ["float16", "bfloat16"])
 def test_results_in_16_bits(dev, kind, shapes, kept):
@@ -72,9 +72,13 @@ def test_results_in_16_bits(dev, kind, shapes, kept):
     for m in ms:
         view(torch, x, m).copy_(make(torch, gen, m.rows, m.cols))
     got = torch.full_like(x, -7.0)
-    f.orthogonal(x, got, listing, dev.workspace(f.workspace_bytes_orthogonal(listing)))
+    ws = dev.workspace(f.workspace_bytes_orthogonal(listing))
+    f.orthogonal(x, got, listing, ws)
+    wide = torch.full((total,), -7.0, device="cuda")
+    f.orthogonal(x, wide, listing, ws)
+    assert torch.equal(wide.to(x.dtype), got)
     for m in ms:
-        near, share = share_allowed(torch, view(torch, x, m), DEFAULT, x.dtype, phases=(1,) if low(m) else (1, 2, 3),
+        near, share = share_allowed(torch, view(torch, x, m), DEFAULT, x.dtype, phases=(1,) if low(m) else (1, 2),
                                     roundings=3 if max(min(s) for s in shapes) > 256 else 1, gain=m.gain)
         other = float((view(torch, got, m) != near).double().mean())
         assert other <= share, (m.rows, m.cols, other, share)
