@@ -1547,8 +1547,9 @@ bool step_bounds(const float* coefficients, int nsteps, int phase_steps, StepBou
 
 namespace {
 
-// A list's matrices under kFineHeight and the others: one part behind the other, in the same workspace.  All in one list of
-// phases of one step, ResNet-50's 54 matrices take 1257 us and so 1188; AlexNet's eight, with two steps for all, 10.83 ms and so 10.95.
+// A list's matrices under kFineHeight and the others: one part behind the other, in the same workspace.  All together, with
+// phases as long as the list's height allows, the matrices of ResNet-50 take 1270 us and so 1283, AlexNet's 10.91 ms and so
+// 11.02, but those under it are then as far off as phases of two steps leave them.
 struct Parts {
     std::vector<MatrixSpan> held;  // where there are both
     const MatrixSpan* m[2];
