@@ -1547,9 +1547,9 @@ bool step_bounds(const float* coefficients, int nsteps, int phase_steps, StepBou
 
 namespace {
 
-// A list's matrices under kFineHeight and the others: one part behind the other, in the same workspace.  All together, with
-// phases as long as the list's height allows, the matrices of ResNet-50 take 1270 us and so 1283, AlexNet's 10.91 ms and so
-// 11.02, but those under it are then as far off as phases of two steps leave them.
+// A list's matrices under kFineHeight and the others: one part behind the other, in the same workspace.  All together,
+// ResNet-50's take 1270 us in phases of one step and so 1283, AlexNet's 10.91 ms in phases of two, which leave the lower ones
+// further off, and so 11.02.
 struct Parts {
     std::vector<MatrixSpan> held;  // where there are both
     const MatrixSpan* m[2];
